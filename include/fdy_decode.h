@@ -1,0 +1,135 @@
+/*
+ * fdy_decode.h - operators of a decode step over a paged key-value cache, for MI355X (gfx950), C ABI.
+ *
+ * What the captured decode graphs of a serving engine hold at every layer (Section 2.1: one graph per batch size;
+ * Section 4.1.1: the KV cache is one of the allocations that the deterministic layout places): rotary positions with the
+ * append of keys and values to their pages, attention of one new token of every sequence over its pages, and, once a
+ * step, the keeping of the pages themselves.  They are made to be captured and restored by the calls of fdy.h:
+ *   - every kernel of a step takes ONE argument, a plain struct of FDY_DECODE_ARG_BYTES bytes whose pointers lie at
+ *     multiples of 8 bytes, so that fdy_scan_pointers finds them in its argument buffer and fdy_materialize /
+ *     fdy_scan_rebase move them to a new layout (fdy_rope_table, which is called once, is not meant);
+ *   - grids follow from host sizes alone (rows, heads, capacity), lengths are read on the device: a captured launch
+ *     stays right while the sequences grow;
+ *   - nothing is read back to the host, nothing is allocated, no memory is cleared by a memset.
+ *
+ * The conventions of fdy.h hold: d_* / device pointers inside the descriptors are the caller's, descriptors are HOST
+ * structs that are read during the call only, calls only enqueue, return codes and status bits are those of fdy.h.  What
+ * only the device can see (a length, a page number, a row number out of range) raises FDY_ST_BAD_INDEX and is skipped as
+ * stated at each call.  Unless stated otherwise arrays that a call writes do not overlap arrays that it reads.
+ */
+#ifndef FDY_DECODE_H
+#define FDY_DECODE_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "fdy.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define FDY_DECODE_ARG_BYTES 512u /* bytes of every kernel's argument */
+
+/* ---- element types -------------------------------------------------------------------- */
+#define FDY_BF16 0u /* bfloat16                                                               */
+#define FDY_F16 1u  /* IEEE half                                                              */
+#define FDY_F8 2u   /* 8-bit e4m3 (OCP: no infinities, largest 448); caches only              */
+
+/* One layer's keys and values in pages.  Token `i` of page `p`, head `h`, starts at element
+ *   p * page_stride + i * token_stride + h * head_stride
+ * of k and of v, and its head_dim elements are contiguous; so both [page][token][head][dim] and
+ * [page][head][token][dim] are served.  An F8 element x stands for x * scale[h].
+ *   page_tokens  a power of two, at most 65,536
+ *   head_dim     1 to 256 (see the calls for what they take)
+ *   a page's elements span less than 2^31 bytes; n_pages < 2^31 */
+typedef struct {
+  void* k;
+  void* v;
+  const float* k_scale; /* [n_heads] device, F8 only; NULL: 1 */
+  const float* v_scale;
+  uint64_t page_stride, token_stride, head_stride; /* elements */
+  uint32_t type;                                   /* FDY_BF16, FDY_F16 or FDY_F8 */
+  uint32_t n_pages, page_tokens, n_heads, head_dim;
+  uint32_t reserved; /* 0 */
+} fdy_kv;            /* 80 B */
+
+/* ---- rotary positions -------------------------------------------------------------------
+ * The angle of pair i of rot_dim / 2 at position p is p * f_i, f_i = base^(-2 i / rot_dim), rescaled for contexts longer
+ * than the trained ones by one of
+ *   FDY_ROPE_PLAIN   f_i
+ *   FDY_ROPE_LINEAR  f_i / factor (positions interpolated)
+ *   FDY_ROPE_NTK     f_i with base * factor^(rot_dim / (rot_dim - 2)); rot_dim >= 4
+ *   FDY_ROPE_YARN    f_i ((1 - g) / factor + g), g = 1 - clamp((i - lo) / (hi - lo), 0, 1), where lo and hi are the (real)
+ *                    pair numbers at which a pair makes `high` and `low` turns over trained_len positions:
+ *                    rot_dim ln(trained_len / (2 pi turns)) / (2 ln base), lo rounded down and hi up, both held
+ *                    within [0, rot_dim - 1], hi = lo + 0.001 where they meet
+ *   FDY_ROPE_BANDS   f_i where trained_len f_i / (2 pi) > high (short waves), f_i / factor where it is < low, and between
+ *                    them f_i ((1 - s) / factor + s) with s = (trained_len f_i / (2 pi) - low) / (high - low)
+ * and cos and sin are multiplied by `magnitude` (1 unless a scheme wants another). */
+#define FDY_ROPE_PLAIN 0u
+#define FDY_ROPE_LINEAR 1u
+#define FDY_ROPE_NTK 2u
+#define FDY_ROPE_YARN 3u
+#define FDY_ROPE_BANDS 4u
+typedef struct {
+  uint32_t scaling;   /* FDY_ROPE_PLAIN ... FDY_ROPE_BANDS */
+  uint32_t rot_dim;   /* even, 2 to 256 */
+  double base;        /* > 1 */
+  double factor;      /* > 0; not read by FDY_ROPE_PLAIN */
+  double low, high;   /* turns, 0 < low < high: FDY_ROPE_YARN, FDY_ROPE_BANDS */
+  double trained_len; /* > 0: FDY_ROPE_YARN, FDY_ROPE_BANDS */
+  double magnitude;   /* finite */
+} fdy_rope;           /* 56 B */
+
+/* Writes d_table[p][0][i] = magnitude cos((first + p) f_i), d_table[p][1][i] = magnitude sin(...) for 0 <= p < n_positions,
+ * i < rot_dim / 2: what fdy_rope_append reads, made once.  Angles are worked out in 64 bits (in 32 a position of a million
+ * would be 0.06 radians off), the table holds 32.  d_table 16-byte aligned; first + n_positions <= 2^31.
+ * FDY_ERR_INVALID_ARG: a field out of the ranges above, a null or misaligned pointer. */
+int fdy_rope_table(const fdy_rope* h_rope, uint64_t first, uint32_t n_positions, float* d_table, void* hip_stream);
+
+/* The frequencies f_i that the table is made of (host; h_freq[rot_dim / 2]). */
+int fdy_rope_frequencies(const fdy_rope* h_rope, double* h_freq);
+
+/* ---- rotary positions + append to the pages ---------------------------------------------
+ * For token t: the first rot_dim elements of every query and key head are turned by the table's row positions[t],
+ *   FDY_ROPE_HALF         pairs (x_i, x_{i + rot_dim/2})
+ *   FDY_ROPE_INTERLEAVED  pairs (x_{2i}, x_{2i+1})
+ *   (x, y) -> (x cos - y sin, y cos + x sin),
+ * the others are copied; queries go to q_out, keys to k_out (if not NULL) and, with the values, to the cache at
+ * slots[t] = page * page_tokens + place.  Worked out in 32 bits, each result rounded once to the type it is stored in (to
+ * nearest, ties to even; F8 saturates at +-448, NaN stays NaN).
+ *   n_tokens at most 2^23.
+ *   A position outside [0, n_positions) leaves the whole token out and raises FDY_ST_BAD_INDEX.
+ *   slots[t] = -1: no cache is written for t (rows that pad a captured batch); any other slot outside the cache: the same,
+ *   and FDY_ST_BAD_INDEX.  Two tokens with one slot: the cache holds either's element by element.
+ *   q NULL: no queries.  slots NULL: no cache is written (kv.k, kv.v may be NULL, v is not read).
+ *   q_out may be q and k_out may be k with the same strides (in place).
+ * Token strides, head strides: in elements; a head's head_dim elements are contiguous.  kv.head_dim, kv.n_heads give the
+ * heads' size and the number of key heads also where no cache is written; kv.type is `type` or FDY_F8.  Any head_dim up to
+ * 256 and any even rot_dim up to it are served; rot_dim a multiple of 16, head_dim of 8, and pointers and strides at
+ * multiples of 16 bytes (8 elements) take wide accesses. */
+#define FDY_ROPE_HALF 0u
+#define FDY_ROPE_INTERLEAVED 1u
+typedef struct {
+  const void* q; /* [n_tokens][n_q_heads][head_dim] or NULL */
+  const void* k; /* [n_tokens][kv.n_heads][head_dim]        */
+  const void* v;
+  void* q_out;
+  void* k_out;              /* or NULL */
+  const int32_t* positions; /* [n_tokens] */
+  const float* table;       /* fdy_rope_table's, [n_positions][2][rot_dim / 2], 16-byte aligned */
+  const int64_t* slots;     /* [n_tokens] or NULL */
+  uint64_t q_token, q_head, k_token, k_head, v_token, v_head;     /* strides */
+  uint64_t q_out_token, q_out_head, k_out_token, k_out_head;
+  fdy_kv kv;
+  uint32_t n_tokens, n_q_heads, n_positions, rot_dim;
+  uint32_t type;   /* FDY_BF16 or FDY_F16 */
+  uint32_t layout; /* FDY_ROPE_HALF or FDY_ROPE_INTERLEAVED */
+} fdy_append;      /* 248 B */
+int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* FDY_DECODE_H */

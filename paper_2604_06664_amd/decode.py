@@ -1,0 +1,113 @@
+"""Binding of include/fdy_decode.h (operators of a decode step over a paged cache): same names, marshalling only.
+
+The descriptors are made once by the make_* helpers from the tensors that they describe (shapes and strides are
+taken from them; the caller keeps the tensors alive) and handed to every call."""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import FDY_ERR_INVALID_ARG, FDY_ERR_WORKSPACE, FDY_OK, FdyError, _check, _ptr, _stream, lib  # noqa: F401
+
+FDY_BF16, FDY_F16, FDY_F8 = 0, 1, 2
+FDY_ROPE_PLAIN, FDY_ROPE_LINEAR, FDY_ROPE_NTK, FDY_ROPE_YARN, FDY_ROPE_BANDS = range(5)
+FDY_ROPE_HALF, FDY_ROPE_INTERLEAVED = 0, 1
+FDY_DECODE_ARG_BYTES = 512
+
+TYPES = dict(bf16=FDY_BF16, f16=FDY_F16, f8=FDY_F8)
+LAYOUTS = dict(half=FDY_ROPE_HALF, interleaved=FDY_ROPE_INTERLEAVED)
+
+
+def _struct(name, pointers=(), u64=(), middle=(), u32=()):
+    fields = [(n, C.c_void_p) for n in pointers] + [(n, C.c_uint64) for n in u64] + list(middle)
+    return type(name, (C.Structure,), dict(_fields_=fields + [(n, C.c_uint32) for n in u32]))
+
+
+fdy_kv = _struct("fdy_kv", ("k", "v", "k_scale", "v_scale"), ("page_stride", "token_stride", "head_stride"), (),
+                 ("type", "n_pages", "page_tokens", "n_heads", "head_dim", "reserved"))
+fdy_append = _struct("fdy_append", ("q", "k", "v", "q_out", "k_out", "positions", "table", "slots"),
+                     ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "q_out_token", "q_out_head",
+                      "k_out_token", "k_out_head"), [("kv", fdy_kv)],
+                     ("n_tokens", "n_q_heads", "n_positions", "rot_dim", "type", "layout"))
+
+
+class fdy_rope(C.Structure):
+    _fields_ = [("scaling", C.c_uint32), ("rot_dim", C.c_uint32)] + [
+        (n, C.c_double) for n in ("base", "factor", "low", "high", "trained_len", "magnitude")]
+
+
+_lib = None
+
+
+def _L():
+    global _lib
+    if _lib is None:
+        L = lib()
+        p, u, z, i = C.c_void_p, C.c_uint32, C.c_size_t, C.c_int
+        for name, result, args in (
+                ("fdy_rope_frequencies", i, [p, p]),
+                ("fdy_rope_table", i, [p, C.c_uint64, u, p, p]),
+                ("fdy_rope_append", i, [p, p, p])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = result, args
+        _lib = L
+    return _lib
+
+
+def _d(desc):
+    return None if desc is None else C.addressof(desc)
+
+
+# ---- descriptors ------------------------------------------------------------------------------
+def type_of(tensor):
+    """FDY_BF16 / FDY_F16 / FDY_F8 of a torch tensor."""
+    return {"torch.bfloat16": FDY_BF16, "torch.float16": FDY_F16, "torch.float8_e4m3fn": FDY_F8}[str(tensor.dtype)]
+
+
+def make_rope(rot_dim, base=10000.0, scaling=FDY_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, trained_len=4096.0,
+              magnitude=1.0):
+    return fdy_rope(scaling, rot_dim, base, factor, low, high, trained_len, magnitude)
+
+
+def make_kv(k, v, *, type, n_pages, page_tokens, n_heads, head_dim, page_stride, token_stride, head_stride,
+            k_scale=None, v_scale=None):
+    """k, v: device pools (tensors or addresses) or None; strides in elements."""
+    return fdy_kv(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), page_stride, token_stride, head_stride, type, n_pages,
+                  page_tokens, n_heads, head_dim, 0)
+
+
+def make_append_desc(*, q, k, v, q_out, positions, table, kv, rot_dim, slots=None, k_out=None, layout=FDY_ROPE_HALF):
+    """q, k, v, q_out, k_out: tensors [tokens, heads, dim] with contiguous last dimension; table [positions, 2, rot_dim / 2]."""
+    d = fdy_append()
+    for name, x in (("q", q), ("k", k), ("v", v), ("q_out", q_out), ("k_out", k_out)):
+        setattr(d, name, _ptr(x))
+        if x is not None:
+            if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+                raise ValueError(f"{name}: [tokens, heads, dim] with contiguous last dimension is wanted")
+            setattr(d, name + "_token", x.stride(0))
+            setattr(d, name + "_head", x.stride(1))
+    d.positions, d.table, d.slots = _ptr(positions), _ptr(table), _ptr(slots)
+    d.kv, d.n_tokens, d.n_q_heads = kv, k.shape[0], 0 if q is None else q.shape[1]
+    d.n_positions, d.rot_dim, d.type, d.layout = table.shape[0], rot_dim, type_of(k), layout
+    return d
+
+
+# ---- entry points (names as in include/fdy_decode.h) --------------------------------------------
+def fdy_rope_frequencies(h_rope, check=True):
+    """-> (rc, host array of rot_dim / 2 frequencies)."""
+    import numpy as np
+
+    f = np.zeros(max(1, h_rope.rot_dim // 2), np.float64)
+    rc = _L().fdy_rope_frequencies(_d(h_rope), _ptr(f))
+    if check:
+        _check(rc, "fdy_rope_frequencies")
+    return rc, f
+
+
+def fdy_rope_table(h_rope, first, n_positions, d_table, stream=None, check=True):
+    rc = _L().fdy_rope_table(_d(h_rope), int(first), int(n_positions), _ptr(d_table), _stream(stream))
+    return _check(rc, "fdy_rope_table") if check else rc
+
+
+def fdy_rope_append(h_desc, d_status=None, stream=None, check=True):
+    rc = _L().fdy_rope_append(_d(h_desc), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_rope_append") if check else rc

@@ -1,0 +1,74 @@
+"""What the decode operators refuse, and their host-side sizes (no GPU call is made before these return)."""
+import ctypes as C
+
+import pytest
+
+from paper_2604_06664_amd import FDY_ERR_INVALID_ARG, FDY_ERR_WORKSPACE, FDY_OK
+from paper_2604_06664_amd import decode as fdd
+
+A = 0x10000  # an address that is aligned and never touched
+
+
+def kv(**kw):
+    f = dict(type=fdd.FDY_BF16, n_pages=4, page_tokens=16, n_heads=2, head_dim=64, page_stride=16 * 128, token_stride=128,
+             head_stride=64)
+    f.update(kw)
+    return fdd.make_kv(f.pop("k", A), f.pop("v", A), **f)
+
+
+def changed(desc, **kw):
+    d = type(desc).from_buffer_copy(desc)
+    for name, value in kw.items():
+        setattr(d, name, value)
+    return d
+
+
+def append(**kw):
+    d = fdd.fdy_append(q=A, k=A, v=A, q_out=A + 0x1000, k_out=None, positions=A, table=A, slots=A, q_token=256, q_head=64,
+                       k_token=128, k_head=64, v_token=128, v_head=64, q_out_token=256, q_out_head=64, kv=kv(), n_tokens=3,
+                       n_q_heads=4, n_positions=10, rot_dim=64, type=fdd.FDY_BF16, layout=fdd.FDY_ROPE_HALF)
+    return changed(d, **kw)
+
+
+BAD_KV = [dict(type=3), dict(page_tokens=0), dict(page_tokens=24), dict(page_tokens=1 << 17), dict(n_heads=0),
+          dict(head_dim=0), dict(head_dim=264), dict(n_pages=0), dict(n_pages=1 << 31), dict(token_stride=1 << 31),
+          dict(head_stride=1 << 40), dict(token_stride=(1 << 31) - 1), dict(page_stride=1 << 41)]
+
+
+def test_sizes_of_the_structs():
+    assert [C.sizeof(s) for s in (fdd.fdy_kv, fdd.fdy_rope, fdd.fdy_append)] == [80, 56, 248]
+
+
+@pytest.mark.parametrize("kw", BAD_KV + [dict(type=fdd.FDY_F16), dict(k=None), dict(v=None), dict(k=A + 1)])
+def test_append_refuses_caches(kw):
+    assert fdd.fdy_rope_append(append(kv=kv(**kw)), stream=0, check=False) == FDY_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [
+    dict(type=fdd.FDY_F8), dict(type=7), dict(layout=2), dict(rot_dim=0), dict(rot_dim=63), dict(rot_dim=66), dict(k=None),
+    dict(positions=None), dict(table=None), dict(table=A + 4), dict(positions=A + 2), dict(slots=A + 4), dict(v=None),
+    dict(q_out=None), dict(n_q_heads=0), dict(n_q_heads=65537), dict(q=A + 1), dict(k_out=A + 1), dict(n_tokens=(1 << 23) + 1),
+    dict(q_out=A, q_out_head=128), dict(k_out=A, k_out_token=64)])
+def test_append_refuses(kw):
+    assert fdd.fdy_rope_append(append(**kw), stream=0, check=False) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_rope_append(None, stream=0, check=False) == FDY_ERR_INVALID_ARG
+
+
+def test_append_of_nothing_is_fine():
+    assert fdd.fdy_rope_append(append(n_tokens=0, k=None, positions=None), stream=0) == FDY_OK
+
+
+def test_rope_refuses():
+    ok = dict(rot_dim=64, base=1e4, scaling=fdd.FDY_ROPE_YARN, factor=4.0, low=1.0, high=32.0, trained_len=4096.0, magnitude=1.0)
+    assert fdd.fdy_rope_frequencies(fdd.make_rope(**ok))[0] == FDY_OK
+    nan, inf = float("nan"), float("inf")
+    for kw in (dict(rot_dim=0), dict(rot_dim=7), dict(rot_dim=258), dict(scaling=5), dict(base=1.0), dict(base=nan), dict(base=inf),
+               dict(factor=0.0), dict(factor=nan), dict(low=0.0), dict(high=1.0), dict(high=nan), dict(trained_len=0.0),
+               dict(trained_len=inf), dict(magnitude=nan), dict(scaling=fdd.FDY_ROPE_NTK, rot_dim=2)):
+        assert fdd.fdy_rope_frequencies(fdd.make_rope(**{**ok, **kw}), check=False)[0] == FDY_ERR_INVALID_ARG, kw
+        assert fdd.fdy_rope_table(fdd.make_rope(**{**ok, **kw}), 0, 4, A, stream=0, check=False) == FDY_ERR_INVALID_ARG, kw
+    rope = fdd.make_rope(64)
+    assert fdd.fdy_rope_table(rope, 0, 4, None, stream=0, check=False) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_rope_table(rope, 0, 4, A + 4, stream=0, check=False) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_rope_table(rope, 1 << 31, 1, A, stream=0, check=False) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_rope_table(rope, 1 << 31, 0, None, stream=0, check=False) == FDY_OK
