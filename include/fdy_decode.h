@@ -129,6 +129,44 @@ typedef struct {
 } fdy_append;      /* 248 B */
 int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stream);
 
+/* ---- attention of one new token over the pages -------------------------------------------
+ * For sequence s with row r = rows[s] (s where rows is NULL), n = lens[r] tokens of which token t lies in page
+ * table[r][t / page_tokens], and query head h (of cache head h / (n_q_heads / kv.n_heads)):
+ *   x_t = scale * q_h . k_t            over t in [max(0, n - window), n)     (window 0: all)
+ *   out_h = sum_t e^(x_t) v_t / sum_t e^(x_t),   lse_h = ln sum_t e^(x_t)
+ * No tokens (or all x_t minus infinity): out 0, lse minus infinity.  Products are of the stored types (F8 widened
+ * exactly), sums, maxima and the joining of parts are held in 32 bits; e^(x_t - max) is rounded to `type` for its product
+ * with v, out once at the end.  What lies in pages behind the row's length is not read.
+ *   lens outside [0, row_pages * page_tokens]: held within, FDY_ST_BAD_INDEX; rows outside [0, n_rows): as no tokens, and
+ *   FDY_ST_BAD_INDEX; a page number outside [0, kv.n_pages): its tokens are left out, FDY_ST_BAD_INDEX.
+ * The results do not depend on what else is in the batch except in the rounding of joined parts, and are the same every
+ * time for the same call.
+ *   q, out, kv.k, kv.v 16-byte aligned, strides multiples of 8 elements (kv's of 16 bytes); head_dim a multiple of 8
+ *   (of 16 with F8) up to 256; n_q_heads a multiple of kv.n_heads; kv.type is `type` or FDY_F8; n_seqs <= 65,536,
+ *   n_q_heads <= 65,536, n_seqs * n_q_heads <= 2^22, row_pages * page_tokens < 2^31.
+ *   workspace  device, 256-byte aligned, fdy_paged_attention_workspace_bytes() (0: a field out of range).  The caller
+ *              clears it once, before its first use; every call leaves what it needs cleared cleared.  Calls that share one
+ *              must not overlap in time, and after FDY_ERR_HIP it is cleared again.  One sized for a descriptor serves
+ *              every one with no more sequences and the same heads and head_dim, on that device. */
+typedef struct {
+  const void* q;        /* [n_seqs][n_q_heads][head_dim] */
+  void* out;            /* [n_seqs][n_q_heads][head_dim] */
+  float* lse;           /* [n_seqs][n_q_heads] or NULL   */
+  const int32_t* table; /* [n_rows][row_pages]           */
+  const int32_t* lens;  /* [n_rows]                      */
+  const int32_t* rows;  /* [n_seqs] or NULL              */
+  uint64_t q_seq, q_head, out_seq, out_head; /* strides  */
+  fdy_kv kv;
+  float scale;
+  uint32_t window; /* 0: none */
+  uint32_t n_seqs, n_q_heads, n_rows, row_pages;
+  uint32_t type; /* FDY_BF16 or FDY_F16 */
+  uint32_t reserved;
+} fdy_attend; /* 192 B */
+size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h_desc);
+int fdy_paged_attention(const fdy_attend* h_desc, void* d_workspace, size_t workspace_bytes, uint32_t* d_status,
+                        void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

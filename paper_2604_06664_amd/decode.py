@@ -28,6 +28,9 @@ fdy_append = _struct("fdy_append", ("q", "k", "v", "q_out", "k_out", "positions"
                      ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "q_out_token", "q_out_head",
                       "k_out_token", "k_out_head"), [("kv", fdy_kv)],
                      ("n_tokens", "n_q_heads", "n_positions", "rot_dim", "type", "layout"))
+fdy_attend = _struct("fdy_attend", ("q", "out", "lse", "table", "lens", "rows"), ("q_seq", "q_head", "out_seq", "out_head"),
+                     [("kv", fdy_kv), ("scale", C.c_float)],
+                     ("window", "n_seqs", "n_q_heads", "n_rows", "row_pages", "type", "reserved"))
 
 
 class fdy_rope(C.Structure):
@@ -46,7 +49,9 @@ def _L():
         for name, result, args in (
                 ("fdy_rope_frequencies", i, [p, p]),
                 ("fdy_rope_table", i, [p, C.c_uint64, u, p, p]),
-                ("fdy_rope_append", i, [p, p, p])):
+                ("fdy_rope_append", i, [p, p, p]),
+                ("fdy_paged_attention_workspace_bytes", z, [p]),
+                ("fdy_paged_attention", i, [p, p, z, p, p])):
             f = getattr(L, name)
             f.restype, f.argtypes = result, args
         _lib = L
@@ -91,6 +96,17 @@ def make_append_desc(*, q, k, v, q_out, positions, table, kv, rot_dim, slots=Non
     return d
 
 
+def make_attend_desc(*, q, out, table, lens, kv, scale, lse=None, rows=None, window=0):
+    """q, out: tensors [sequences, heads, dim] with contiguous last dimension; table [rows, pages] and lens, 32-bit."""
+    for name, x in (("q", q), ("out", out)):
+        if x.dim() != 3 or x.stride(2) != 1:
+            raise ValueError(f"{name}: [sequences, heads, dim] with contiguous last dimension is wanted")
+    d = fdy_attend(_ptr(q), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), _ptr(rows), q.stride(0), q.stride(1),
+                   out.stride(0), out.stride(1), kv, scale, window, q.shape[0], q.shape[1], table.shape[0],
+                   table.shape[1], type_of(q), 0)
+    return d
+
+
 # ---- entry points (names as in include/fdy_decode.h) --------------------------------------------
 def fdy_rope_frequencies(h_rope, check=True):
     """-> (rc, host array of rot_dim / 2 frequencies)."""
@@ -111,3 +127,12 @@ def fdy_rope_table(h_rope, first, n_positions, d_table, stream=None, check=True)
 def fdy_rope_append(h_desc, d_status=None, stream=None, check=True):
     rc = _L().fdy_rope_append(_d(h_desc), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_rope_append") if check else rc
+
+
+def fdy_paged_attention_workspace_bytes(h_desc):
+    return _L().fdy_paged_attention_workspace_bytes(_d(h_desc))
+
+
+def fdy_paged_attention(h_desc, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    rc = _L().fdy_paged_attention(_d(h_desc), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_paged_attention") if check else rc

@@ -35,8 +35,14 @@ BAD_KV = [dict(type=3), dict(page_tokens=0), dict(page_tokens=24), dict(page_tok
           dict(head_stride=1 << 40), dict(token_stride=(1 << 31) - 1), dict(page_stride=1 << 41)]
 
 
+def attend(**kw):
+    d = fdd.fdy_attend(q=A, out=A, lse=A, table=A, lens=A, rows=None, q_seq=256, q_head=64, out_seq=256, out_head=64, kv=kv(),
+                       scale=0.125, window=0, n_seqs=3, n_q_heads=4, n_rows=3, row_pages=5, type=fdd.FDY_BF16)
+    return changed(d, **kw)
+
+
 def test_sizes_of_the_structs():
-    assert [C.sizeof(s) for s in (fdd.fdy_kv, fdd.fdy_rope, fdd.fdy_append)] == [80, 56, 248]
+    assert [C.sizeof(s) for s in (fdd.fdy_kv, fdd.fdy_rope, fdd.fdy_append, fdd.fdy_attend)] == [80, 56, 248, 192]
 
 
 @pytest.mark.parametrize("kw", BAD_KV + [dict(type=fdd.FDY_F16), dict(k=None), dict(v=None), dict(k=A + 1)])
@@ -72,3 +78,36 @@ def test_rope_refuses():
     assert fdd.fdy_rope_table(rope, 0, 4, A + 4, stream=0, check=False) == FDY_ERR_INVALID_ARG
     assert fdd.fdy_rope_table(rope, 1 << 31, 1, A, stream=0, check=False) == FDY_ERR_INVALID_ARG
     assert fdd.fdy_rope_table(rope, 1 << 31, 0, None, stream=0, check=False) == FDY_OK
+
+
+@pytest.mark.parametrize("kw", [dict(kv=kv(**k)) for k in BAD_KV + [dict(type=fdd.FDY_F16), dict(head_dim=60)]] + [
+    dict(kv=kv(type=fdd.FDY_F8, head_dim=72)), dict(type=2), dict(reserved=1), dict(n_seqs=65537), dict(n_q_heads=0),
+    dict(n_q_heads=5), dict(n_q_heads=65538), dict(n_seqs=65536, n_q_heads=66), dict(row_pages=1 << 27)])
+def test_attention_refuses_sizes(kw):
+    d = attend(**kw)
+    assert fdd.fdy_paged_attention_workspace_bytes(d) == 0
+    assert fdd.fdy_paged_attention(d, A, 1 << 40, stream=0, check=False) == FDY_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [dict(q=None), dict(q=A + 8), dict(out=None), dict(out=A + 2), dict(lse=A + 1), dict(table=None),
+                                dict(lens=None), dict(lens=A + 2), dict(rows=A + 1), dict(kv=kv(k=None)), dict(kv=kv(v=A + 8)),
+                                dict(q_head=60), dict(out_seq=4), dict(kv=kv(token_stride=132)), dict(kv=kv(k_scale=A + 2)),
+                                dict(kv=kv(type=fdd.FDY_F8, token_stride=136))])
+def test_attention_refuses_pointers_and_strides(kw):
+    assert fdd.fdy_paged_attention(attend(**kw), A, 1 << 40, stream=0, check=False) == FDY_ERR_INVALID_ARG
+
+
+def test_attention_workspace():
+    d = attend()
+    n = fdd.fdy_paged_attention_workspace_bytes(d)
+    assert 0 < n < 32 << 20 and n % 256 == 0
+    for ws, size in ((None, n), (A + 128, n), (A, n - 1)):
+        assert fdd.fdy_paged_attention(d, ws, size, stream=0, check=False) == FDY_ERR_WORKSPACE
+    last = n
+    for seqs in (4, 100, 200, 1000, 65536 // 2):  # one made for more sequences serves fewer
+        m = fdd.fdy_paged_attention_workspace_bytes(attend(n_seqs=seqs))
+        assert m >= last
+        last = m
+    assert fdd.fdy_paged_attention(attend(n_seqs=0, q=None), None, 0, stream=0) == FDY_OK
+    assert fdd.fdy_paged_attention(None, A, n, stream=0, check=False) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_paged_attention_workspace_bytes(None) == 0
