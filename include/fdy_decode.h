@@ -167,6 +167,74 @@ size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h_desc);
 int fdy_paged_attention(const fdy_attend* h_desc, void* d_workspace, size_t workspace_bytes, uint32_t* d_status,
                         void* hip_stream);
 
+/* ---- keeping the pages --------------------------------------------------------------------
+ * A pool of n_pages pages that rows of pages share.  Its books are device arrays of the caller's:
+ *   refs[p]       rows that hold page p (a row that holds it twice counts twice)
+ *   free_bits     bit p of the array is set iff refs[p] == 0 (bits from n_pages on are clear)
+ *   table[r][j]   page that holds tokens [j * page_tokens, (j+1) * page_tokens) of row r, for j < ceil(lens[r] / page_tokens);
+ *                 what lies behind is not read
+ *   lens[r]       tokens of row r
+ * and its contents are n_planes areas (keys and values of every layer): page p of plane i is page_bytes bytes at
+ * planes[i] + p * page_stride.  planes[i] are device addresses, in a device array; n_planes 0: books only.
+ * Everything below is deterministic: pages are taken lowest number first, in the order of the list of rows.
+ * Books that contradict each other (or lists with a row twice) give unspecified books, with no access out of bounds:
+ * page and row numbers and lengths out of range are skipped and raise FDY_ST_BAD_INDEX; of entries with the same row to
+ * be written the first counts, the others are skipped with FDY_ST_BAD_INDEX.
+ *   refs, table, lens, rows 4-byte, free_bits, planes, slots 8-byte aligned; planes' addresses, page_bytes, page_stride
+ *   multiples of 16; page_tokens a power of two up to 65,536; n_pages, n_rows <= 2^28, row_pages <= 2^25,
+ *   row_pages * page_tokens < 2^31, n_planes <= 2^20 */
+typedef struct {
+  uint32_t* refs;      /* [n_pages]              */
+  uint64_t* free_bits; /* [ceil(n_pages / 64)]   */
+  int32_t* table;      /* [n_rows][row_pages]    */
+  int32_t* lens;       /* [n_rows]               */
+  const uint64_t* planes; /* [n_planes] addresses, or NULL */
+  uint64_t page_bytes, page_stride;
+  uint32_t n_pages, page_tokens, n_rows, row_pages, n_planes;
+  uint32_t reserved;
+} fdy_pages; /* 80 B */
+
+/* All pages free, all rows empty. */
+int fdy_pages_reset(const fdy_pages* h_pages, void* hip_stream);
+
+/* Workspace (device, 256-byte aligned, contents irrelevant) of the calls below for lists of up to n entries; 0: a field
+ * out of range.  Calls that share one must not overlap in time. */
+size_t fdy_pages_workspace_bytes(const fdy_pages* h_pages, uint32_t n);
+
+/* Room for counts[i] (1 each where counts is NULL) more tokens of row rows[i] (i where rows is NULL), i < n: new pages are
+ * taken, lens grows, and slots / positions (either may be NULL) receive, packed in the order of the list, where each new
+ * token goes and its number in its row: what fdy_rope_append takes.  A partly filled last page that other rows hold too is
+ * copied first, in all planes, to a page of the row's own; of rows that hold such a page among themselves alone the last in
+ * the list keeps it.
+ *   A row gets all or nothing: one that does not fit its table, or whose pages the pool has not left after all rows before
+ *   it (those that get nothing for want of pages count as well), or whose tokens end behind n_slots, stays as it is, its
+ *   slots are -1 (positions as if), and FDY_ST_CAPACITY is raised.
+ *   counts[i] < 0 counts as 0 and raises FDY_ST_BAD_INDEX.  n <= 65,536; the sum of counts < 2^31. */
+int fdy_pages_extend(const fdy_pages* h_pages, const int32_t* d_rows, const int32_t* d_counts, uint32_t n,
+                     int64_t* d_slots, int32_t* d_positions, uint32_t n_slots, void* d_workspace, size_t workspace_bytes,
+                     uint32_t* d_status, void* hip_stream);
+
+/* Row dst[i] becomes a holder of what row src[i] held before the call, for all i < n at once (a permutation of rows, beams
+ * that go on from other beams); what dst[i] held is given up, pages that nobody holds any more become free.  Entries of
+ * dst[i]'s table behind its new length stay what they were.  No page is copied: fdy_pages_extend does it when a shared
+ * page is to be written.  n <= 65,536 */
+int fdy_pages_fork(const fdy_pages* h_pages, const int32_t* d_src, const int32_t* d_dst, uint32_t n, void* d_workspace,
+                   size_t workspace_bytes, uint32_t* d_status, void* hip_stream);
+
+/* Rows rows[i] give up their pages and become empty.  n <= 65,536 */
+int fdy_pages_free(const fdy_pages* h_pages, const int32_t* d_rows, uint32_t n, uint32_t* d_status, void* hip_stream);
+
+/* The contents of page src[i] to page dst[i] in all planes, i < n; no page may be both, or twice in dst.  The books stay
+ * as they are. */
+int fdy_pages_copy(const fdy_pages* h_pages, const int32_t* d_src, const int32_t* d_dst, uint32_t n, uint32_t* d_status,
+                   void* hip_stream);
+
+/* Moves pages so that the live ones are [0, *d_n_live): the k-th live page from there on goes to the k-th free page below,
+ * with its contents in all planes, and the rows' tables follow.  d_map[n_pages] (may be NULL) receives the new number of
+ * every live page, -1 for the free ones (for page numbers kept elsewhere). */
+int fdy_pages_compact(const fdy_pages* h_pages, int32_t* d_map, uint32_t* d_n_live, void* d_workspace,
+                      size_t workspace_bytes, uint32_t* d_status, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

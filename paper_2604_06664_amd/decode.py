@@ -31,6 +31,8 @@ fdy_append = _struct("fdy_append", ("q", "k", "v", "q_out", "k_out", "positions"
 fdy_attend = _struct("fdy_attend", ("q", "out", "lse", "table", "lens", "rows"), ("q_seq", "q_head", "out_seq", "out_head"),
                      [("kv", fdy_kv), ("scale", C.c_float)],
                      ("window", "n_seqs", "n_q_heads", "n_rows", "row_pages", "type", "reserved"))
+fdy_pages = _struct("fdy_pages", ("refs", "free_bits", "table", "lens", "planes"), ("page_bytes", "page_stride"), (),
+                    ("n_pages", "page_tokens", "n_rows", "row_pages", "n_planes", "reserved"))
 
 
 class fdy_rope(C.Structure):
@@ -51,7 +53,14 @@ def _L():
                 ("fdy_rope_table", i, [p, C.c_uint64, u, p, p]),
                 ("fdy_rope_append", i, [p, p, p]),
                 ("fdy_paged_attention_workspace_bytes", z, [p]),
-                ("fdy_paged_attention", i, [p, p, z, p, p])):
+                ("fdy_paged_attention", i, [p, p, z, p, p]),
+                ("fdy_pages_reset", i, [p, p]),
+                ("fdy_pages_workspace_bytes", z, [p, u]),
+                ("fdy_pages_extend", i, [p, p, p, u, p, p, u, p, z, p, p]),
+                ("fdy_pages_fork", i, [p, p, p, u, p, z, p, p]),
+                ("fdy_pages_free", i, [p, p, u, p, p]),
+                ("fdy_pages_copy", i, [p, p, p, u, p, p]),
+                ("fdy_pages_compact", i, [p, p, p, p, z, p, p])):
             f = getattr(L, name)
             f.restype, f.argtypes = result, args
         _lib = L
@@ -107,6 +116,12 @@ def make_attend_desc(*, q, out, table, lens, kv, scale, lse=None, rows=None, win
     return d
 
 
+def make_pages(*, refs, free_bits, table, lens, page_tokens, planes=None, page_bytes=0, page_stride=0):
+    """refs [pages], table [rows, pages of a row], lens [rows], 32-bit; free_bits, planes (device addresses) 64-bit."""
+    return fdy_pages(_ptr(refs), _ptr(free_bits), _ptr(table), _ptr(lens), _ptr(planes), page_bytes, page_stride,
+                     refs.shape[0], page_tokens, table.shape[0], table.shape[1], 0 if planes is None else planes.shape[0], 0)
+
+
 # ---- entry points (names as in include/fdy_decode.h) --------------------------------------------
 def fdy_rope_frequencies(h_rope, check=True):
     """-> (rc, host array of rot_dim / 2 frequencies)."""
@@ -136,3 +151,41 @@ def fdy_paged_attention_workspace_bytes(h_desc):
 def fdy_paged_attention(h_desc, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
     rc = _L().fdy_paged_attention(_d(h_desc), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_paged_attention") if check else rc
+
+
+def fdy_pages_reset(h_pages, stream=None, check=True):
+    rc = _L().fdy_pages_reset(_d(h_pages), _stream(stream))
+    return _check(rc, "fdy_pages_reset") if check else rc
+
+
+def fdy_pages_workspace_bytes(h_pages, n):
+    return _L().fdy_pages_workspace_bytes(_d(h_pages), int(n))
+
+
+def fdy_pages_extend(h_pages, d_rows, d_counts, n, d_slots, d_positions, n_slots, d_workspace, workspace_bytes,
+                     d_status=None, stream=None, check=True):
+    rc = _L().fdy_pages_extend(_d(h_pages), _ptr(d_rows), _ptr(d_counts), int(n), _ptr(d_slots), _ptr(d_positions),
+                               int(n_slots), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_pages_extend") if check else rc
+
+
+def fdy_pages_fork(h_pages, d_src, d_dst, n, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    rc = _L().fdy_pages_fork(_d(h_pages), _ptr(d_src), _ptr(d_dst), int(n), _ptr(d_workspace), int(workspace_bytes),
+                             _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_pages_fork") if check else rc
+
+
+def fdy_pages_free(h_pages, d_rows, n, d_status=None, stream=None, check=True):
+    rc = _L().fdy_pages_free(_d(h_pages), _ptr(d_rows), int(n), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_pages_free") if check else rc
+
+
+def fdy_pages_copy(h_pages, d_src, d_dst, n, d_status=None, stream=None, check=True):
+    rc = _L().fdy_pages_copy(_d(h_pages), _ptr(d_src), _ptr(d_dst), int(n), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_pages_copy") if check else rc
+
+
+def fdy_pages_compact(h_pages, d_map, d_n_live, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    rc = _L().fdy_pages_compact(_d(h_pages), _ptr(d_map), _ptr(d_n_live), _ptr(d_workspace), int(workspace_bytes),
+                                _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_pages_compact") if check else rc

@@ -41,8 +41,14 @@ def attend(**kw):
     return changed(d, **kw)
 
 
+def pages(**kw):
+    d = fdd.fdy_pages(refs=A, free_bits=A, table=A, lens=A, planes=A, page_bytes=4096, page_stride=4096, n_pages=100,
+                      page_tokens=16, n_rows=8, row_pages=10, n_planes=4)
+    return changed(d, **kw)
+
+
 def test_sizes_of_the_structs():
-    assert [C.sizeof(s) for s in (fdd.fdy_kv, fdd.fdy_rope, fdd.fdy_append, fdd.fdy_attend)] == [80, 56, 248, 192]
+    assert [C.sizeof(s) for s in (fdd.fdy_kv, fdd.fdy_rope, fdd.fdy_append, fdd.fdy_attend, fdd.fdy_pages)] == [80, 56, 248, 192, 80]
 
 
 @pytest.mark.parametrize("kw", BAD_KV + [dict(type=fdd.FDY_F16), dict(k=None), dict(v=None), dict(k=A + 1)])
@@ -111,3 +117,68 @@ def test_attention_workspace():
     assert fdd.fdy_paged_attention(attend(n_seqs=0, q=None), None, 0, stream=0) == FDY_OK
     assert fdd.fdy_paged_attention(None, A, n, stream=0, check=False) == FDY_ERR_INVALID_ARG
     assert fdd.fdy_paged_attention_workspace_bytes(None) == 0
+
+
+CONTENTS, WORKSPACE = ("extend", "copy", "compact"), ("extend", "fork", "compact")
+ALL = ("reset", "extend", "fork", "free", "copy", "compact")
+
+
+def page_calls(d, names, ws=A, size=1 << 50):
+    """Return codes of the named calls.  Only calls that have to be refused are made: the addresses are none."""
+    kw = dict(stream=0, check=False)
+    calls = dict(reset=lambda: fdd.fdy_pages_reset(d, **kw),
+                 extend=lambda: fdd.fdy_pages_extend(d, A, A, 3, A, A, 9, ws, size, A, **kw),
+                 fork=lambda: fdd.fdy_pages_fork(d, A, A, 3, ws, size, A, **kw),
+                 free=lambda: fdd.fdy_pages_free(d, A, 3, A, **kw),
+                 copy=lambda: fdd.fdy_pages_copy(d, A, A, 3, A, **kw),
+                 compact=lambda: fdd.fdy_pages_compact(d, A, A, ws, size, A, **kw))
+    return {name: calls[name]() for name in names}
+
+
+@pytest.mark.parametrize("kw", [dict(reserved=1), dict(n_pages=0), dict(n_pages=(1 << 28) + 1), dict(n_rows=(1 << 28) + 1),
+                                dict(page_tokens=0), dict(page_tokens=48), dict(page_tokens=1 << 17), dict(row_pages=(1 << 25) + 1),
+                                dict(row_pages=1 << 24, page_tokens=128), dict(page_bytes=24), dict(page_stride=8),
+                                dict(page_bytes=1 << 41), dict(n_planes=(1 << 20) + 1)])
+def test_pages_refuse_sizes(kw):
+    d = pages(**kw)
+    assert fdd.fdy_pages_workspace_bytes(d, 3) == 0
+    assert set(page_calls(d, ALL).values()) == {FDY_ERR_INVALID_ARG}
+
+
+def test_pages_refuse_pointers():
+    for kw in (dict(refs=None), dict(refs=A + 2), dict(free_bits=None), dict(free_bits=A + 4), dict(lens=None), dict(lens=A + 1),
+               dict(table=None), dict(table=A + 2)):
+        assert set(page_calls(pages(**kw), [n for n in ALL if n != "copy"]).values()) == {FDY_ERR_INVALID_ARG}, kw
+    for kw in (dict(planes=None), dict(planes=A + 4)):
+        assert set(page_calls(pages(**kw), CONTENTS).values()) == {FDY_ERR_INVALID_ARG}, kw
+    assert set(page_calls(None, ALL).values()) == {FDY_ERR_INVALID_ARG}
+    d, k = pages(), dict(stream=0, check=False)
+    for lists in ((A + 2, A, A, A), (A, A + 1, A, A), (A, A, A + 4, A), (A, A, A, A + 2)):
+        assert fdd.fdy_pages_extend(d, lists[0], lists[1], 3, lists[2], lists[3], 9, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_pages_extend(d, None, A, 9, A, A, 9, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG  # more than there are rows
+    assert fdd.fdy_pages_extend(d, A, A, 65537, A, A, 9, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_pages_extend(d, A, A, 3, A, A, 1 << 31, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG
+    for a, b in ((None, A), (A, None), (A + 2, A), (A, A + 2)):
+        assert fdd.fdy_pages_fork(d, a, b, 3, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG
+        assert fdd.fdy_pages_copy(d, a, b, 3, A, **k) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_pages_free(d, None, 3, A, **k) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_pages_free(d, A + 2, 3, A, **k) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_pages_compact(d, A + 2, A, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG
+    assert fdd.fdy_pages_compact(d, A, A + 2, A, 1 << 50, A, **k) == FDY_ERR_INVALID_ARG
+
+
+def test_pages_workspace():
+    d = pages()
+    n = fdd.fdy_pages_workspace_bytes(d, 3)
+    assert n > 0 and n % 256 == 0 and fdd.fdy_pages_workspace_bytes(d, 65537) == 0 and fdd.fdy_pages_workspace_bytes(None, 1) == 0
+    for ws, size in ((None, 1 << 40), (A + 128, 1 << 40), (A, 0)):
+        assert set(page_calls(d, WORKSPACE, ws, size).values()) == {FDY_ERR_WORKSPACE}
+
+
+def test_lists_of_nothing_are_fine():
+    d, k = pages(), dict(stream=0, check=False)
+    assert fdd.fdy_pages_extend(d, None, None, 0, None, None, 0, None, 0, None, **k) == FDY_OK
+    assert fdd.fdy_pages_fork(d, None, None, 0, None, 0, None, **k) == FDY_OK
+    assert fdd.fdy_pages_free(d, None, 0, None, **k) == FDY_OK
+    assert fdd.fdy_pages_copy(d, None, None, 0, None, **k) == FDY_OK
+    assert fdd.fdy_pages_copy(pages(n_planes=0), A, A, 3, None, **k) == FDY_OK
