@@ -147,7 +147,7 @@ int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stre
  *   workspace  device, 256-byte aligned, fdy_paged_attention_workspace_bytes() (0: a field out of range).  The caller
  *              clears it once, before its first use; every call leaves what it needs cleared cleared.  Calls that share one
  *              must not overlap in time, and after FDY_ERR_HIP it is cleared again.  One sized for a descriptor serves
- *              every one with no more sequences and the same heads and head_dim, on that device. */
+ *              every one with no more sequences, no wider tables and the same heads, head_dim and page_tokens. */
 typedef struct {
   const void* q;        /* [n_seqs][n_q_heads][head_dim] */
   void* out;            /* [n_seqs][n_q_heads][head_dim] */

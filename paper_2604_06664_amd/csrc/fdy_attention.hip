@@ -21,15 +21,16 @@ using namespace fdy;
 namespace {
 
 constexpr u32 kWaves = 4, kTile = 32, kCus = 256;
-constexpr u32 kLeast = 8;  // tiles of a piece, at least: two for each wave
+constexpr u32 kLeast = 8;  // tiles of a share, at least: two for each wave
+constexpr u32 kEach = 4;   // what a row costs beside its tiles (queries, join, output), in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArg {
   fdy_attend d;
   u32* status;
   u32* counters;  // [n_seqs][columns], zero between calls
-  float* parts;   // [pieces][columns] of: [rows][head_dim] sums, [rows] maxima, [rows] sums of e; each 16-byte aligned
-  u32 page_shift, group, q_tiles, columns, extra, rows;  // columns: cache heads x q_tiles; rows: query heads of a tile
+  float* parts;   // [shares][columns][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
+  u32 page_shift, group, q_tiles, columns, shares, rows;  // columns: cache heads x q_tiles; rows: query heads of a tile
 };
 typedef Arg<AttendArg> Attend;
 
@@ -78,6 +79,24 @@ __device__ __forceinline__ float over_groups(float x, float (*op)(float, float))
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float plus(float a, float b) { return a + b; }
 
+// Parts go from one workgroup to another, on another die as it may be: they are written through to memory and read from
+// there (device scope on each access), for a fence would write back and drop all that the dies' caches hold, once a wave.
+constexpr int kDeviceScope = 0x10;  // sc1
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t part_buffer(float* part, u64 floats) { return buffer(part, (u32)floats * 4); }
+__device__ __forceinline__ float as_float(u32 v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t part, u32 at, f32x4 x) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), part, at * 4, 0, kDeviceScope);
+}
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t part, u32 at, float x, float y) {
+  const v2u32 w = {__builtin_bit_cast(u32, x), __builtin_bit_cast(u32, y)};
+  __builtin_amdgcn_raw_buffer_store_b64(w, part, at * 4, 0, kDeviceScope);
+}
+__device__ __forceinline__ f32x4 get_part4(__amdgpu_buffer_rsrc_t part, u32 at) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at * 4, 0, kDeviceScope));
+}
+__device__ __forceinline__ v2u32 get_part2(__amdgpu_buffer_rsrc_t part, u32 at) {
+  return __builtin_amdgcn_raw_buffer_load_b64(part, at * 4, 0, kDeviceScope);
+}
 __host__ __device__ inline u32 part_floats(u32 rows, u32 head_dim) { return rows * head_dim + (2 * rows + 3) / 4 * 4; }
 
 // ---- which tokens a workgroup takes -----------------------------------------------------------------
@@ -103,44 +122,59 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 s) {
   return r;
 }
 
-struct Piece {
-  u32 seq, split, n_splits, at;  // `at`: number of the piece
-  bool none;
+// The rows' tiles lie one after the other on a line, kEach places ahead of each row's; equal shares of the line go to the
+// workgroups of a column.  So all of them have the same to do whatever the lengths are, and a row is in as many parts as
+// shares reach into it.
+struct Share {
+  u64 begin, end, per;  // places
+  u32 seq;              // row at `begin`, and where it starts
+  u64 start;
 };
 
-// The pieces of all rows, as equal as whole rows allow: every piece has at most `per` tiles, where
-// sum(ceil(tiles / per)) <= sum(tiles) / per + n_seqs is at most the grid.  Every wave works this out for itself.
-__device__ __forceinline__ Piece piece_of(const Attend& a, u32 at) {
-  const u32 lane = lane_id(), n = a.d.n_seqs;
-  u64 total = 0;
-  for (u32 s0 = 0; s0 < n; s0 += 64) {
-    const u32 s = s0 + lane;
-    const u32 t = s < n ? span_of(a, s).tiles() : 0;
-    const u64 inc = wave_incl_scan((u64)t);
-    total += (u64)__shfl((long long)inc, 63);
+__device__ __forceinline__ u64 share_of(const Attend& a, u64 total) {
+  const u64 per = (total + a.shares - 1) / a.shares;
+  return per < kLeast + kEach ? kLeast + kEach : per;
+}
+
+// All threads of the workgroup; s_share: 6 u64 of LDS.
+__device__ __forceinline__ bool find_share(const Attend& a, u32 at, Share& out, u64* s_share) {
+  const u32 n = a.d.n_seqs, tid = threadIdx.x;
+  if (n == 1) {
+    const u64 total = span_of(a, 0).tiles() + kEach;
+    out.per = share_of(a, total);
+    out.begin = at * out.per;
+    out.end = out.begin + out.per < total ? out.begin + out.per : total;
+    out.seq = 0, out.start = 0;
+    return out.begin < total;
   }
-  u32 per = (u32)((total + a.extra - 1) / a.extra);
-  if (per < kLeast) per = kLeast;
-  Piece p;
-  p.at = at;
-  p.none = true;
-  u32 base = 0;
-  for (u32 s0 = 0; s0 < n; s0 += 64) {
-    const u32 s = s0 + lane;
-    u32 t = s < n ? span_of(a, s).tiles() : 0;
-    u32 k = s < n ? (t > per ? (t + per - 1) / per : 1u) : 0u;
-    const u32 inc = wave_incl_scan(k), sum = (u32)__shfl((int)inc, 63);
-    if (at < base + sum) {
-      const u32 l = (u32)__popcll(ballot(base + inc <= at));
-      p.seq = s0 + l;
-      p.n_splits = (u32)__shfl((int)k, (int)l);
-      p.split = at - (base + (u32)__shfl((int)inc, (int)l) - p.n_splits);
-      p.none = false;
-      return p;
+  const u32 slice = (n + 255) / 256, s0 = tid * slice, s1 = s0 + slice < n ? s0 + slice : n;
+  u64 mine = 0;
+  for (u32 s = s0; s < s1; ++s) mine += span_of(a, s).tiles() + kEach;
+  const u64 inc = wave_incl_scan(mine);
+  if (lane_id() == 63) s_share[tid >> 6] = inc;
+  __syncthreads();
+  u64 before = inc - mine, total = 0;
+#pragma unroll
+  for (u32 w = 0; w < kWaves; ++w) {
+    if (w < tid >> 6) before += s_share[w];
+    total += s_share[w];
+  }
+  out.per = share_of(a, total);
+  out.begin = at * out.per;
+  out.end = out.begin + out.per < total ? out.begin + out.per : total;
+  if (out.begin >= total) return false;
+  if (out.begin >= before && out.begin < before + mine) {
+    u32 s = s0;
+    for (;; ++s) {
+      const u64 cost = span_of(a, s).tiles() + kEach;
+      if (out.begin < before + cost) break;
+      before += cost;
     }
-    base += sum;
+    s_share[4] = s, s_share[5] = before;
   }
-  return p;
+  __syncthreads();
+  out.seq = uniform((u32)s_share[4]), out.start = uniform(s_share[5]);
+  return true;
 }
 
 // ---- loads ------------------------------------------------------------------------------------------
@@ -191,104 +225,121 @@ struct Tile {
   v4u32 k[2][kLoads];
   vword v[8][kParts];
 
-  // The wave's constant offsets
+  // The lane's constant offsets in a page: kNowhere behind head_dim
   struct Lanes {
-    u32 col, grp;
-    u32 k_at[kLoads];  // byte offsets of the lane's pieces of a key row, kNowhere behind head_dim
-    u32 v_at[kParts];
-    u64 k_head, v_head;
+    u32 col, grp, token_bytes;
+    u32 k_at[kLoads], v_at[kParts];
+    u64 head;  // bytes
   };
 
-  static __device__ void lanes(const Attend& a, u32 head, Lanes& z) {
+  static __device__ __forceinline__ void lanes(const Attend& a, u32 head, Lanes& z) {
     const u32 l = lane_id(), D = a.d.kv.head_dim;
     z.col = l & 15, z.grp = l >> 4;
+    z.token_bytes = (u32)a.d.kv.token_stride * kEs;
+    z.head = head * a.d.kv.head_stride * kEs;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const u32 e = (j * 4 + z.grp) * (16 / kEs);
-      z.k_at[j] = e < D ? e * kEs : kNowhere;
+      z.k_at[j] = e < D ? e * kEs + (kSmall ? 0 : z.col * z.token_bytes) : kNowhere;
     }
 #pragma unroll
     for (int j = 0; j < kParts; ++j) {
       const u32 e = j * 16 * kWide + z.col * kWide;
-      z.v_at[j] = e < D ? e * kEs : kNowhere;
+      z.v_at[j] = e < D ? e * kEs + (kSmall ? 0 : z.grp * 4 * z.token_bytes) : kNowhere;
     }
   }
 
-  // Tokens [t, t + 32) of the row; those outside [first, end) read as zero.  Returns which of the two halves have a page.
-  __device__ void load(const Attend& a, const Lanes& z, const Span& span, u32 head, u32 t, bool& bad) {
-    const fdy_kv& c = a.d.kv;
-    const u32 token_bytes = (u32)c.token_stride * kEs;
-    const u64 head_bytes = head * c.head_stride * kEs;
-    const int* table = a.d.table + (u64)span.row * a.d.row_pages;
+  // The pages of tokens [t, t + 32): the wave's two, looked up by scalar loads a tile ahead.  ~0: none to be seen
+  struct Ids {
+    u32 page[2];
+  };
+  static __device__ __forceinline__ Ids ids(const Attend& a, const Span& span, u32 t, bool& bad) {
+    Ids r;
+    if (kSmall) return r;
+    typedef const __attribute__((address_space(4))) u32* table_t;  // no one writes it while the kernel runs
+    const table_t table = (table_t)(uintptr_t)(a.d.table + (u64)span.row * a.d.row_pages);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const u32 t0 = t + u * 16;
-      if (!kSmall) {
-        const bool seen = t0 < span.end && t0 + 16 > span.first;
-        const u32 page = seen ? uniform((u32)table[t0 >> a.page_shift]) : ~0u;
-        const bool in = page < c.n_pages;
-        bad |= seen && !in;
-        const u64 at = in ? page * c.page_stride * kEs + (t0 & (c.page_tokens - 1)) * (u64)token_bytes + head_bytes : 0;
-        const auto rk = buffer((const uint8_t*)c.k + at, kNowhere - 1), rv = buffer((const uint8_t*)c.v + at, kNowhere - 1);
-        const u32 tk = t0 + z.col;
-        const bool ok = in && tk >= span.first && tk < span.end;
+      r.page[u] = ~0u;
+      if (t0 < span.end && t0 + 16 > span.first) {
+        const u32 p = table[t0 >> a.page_shift];
+        if (p < a.d.kv.n_pages)
+          r.page[u] = p;
+        else
+          bad = true;
+      }
+    }
+    return r;
+  }
+
+  static __device__ __forceinline__ u64 place(const Attend& a, const Lanes& z, u32 page, u32 t) {
+    return page * a.d.kv.page_stride * kEs + (t & (a.d.kv.page_tokens - 1)) * (u64)z.token_bytes + z.head;
+  }
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t half(const Attend& a, const Lanes& z, const Ids& ids, int u, u32 t,
+                                                                const void* pool) {
+    return buffer((const uint8_t*)pool + (ids.page[u] != ~0u ? place(a, z, ids.page[u], t + u * 16) : 0), kNowhere - 1);
+  }
+  // Where a lane finds a token of a small page, or null
+  static __device__ __forceinline__ const uint8_t* small(const Attend& a, const Lanes& z, const Span& span, u32 t, const void* pool,
+                                                         bool& bad) {
+    if (t - span.first >= span.end - span.first) return nullptr;
+    const u32 page = (u32)a.d.table[(u64)span.row * a.d.row_pages + (t >> a.page_shift)];
+    if (page >= a.d.kv.n_pages) {
+      bad = true;
+      return nullptr;
+    }
+    return (const uint8_t*)pool + place(a, z, page, t);
+  }
+
+  // Keys, then values of tokens [t, t + 32); those outside the span read as zero (so do all, at a `t` behind it).
+  __device__ __forceinline__ void load_k(const Attend& a, const Lanes& z, const Span& span, const Ids& ids, u32 t, bool& bad) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-          k[u][j] = Word<16>::load(rk, ok && z.k_at[j] != kNowhere ? z.k_at[j] + z.col * token_bytes : kNowhere, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32 tv = t0 + z.grp * 4 + i;
-          const bool okv = in && tv >= span.first && tv < span.end;
-#pragma unroll
-          for (int j = 0; j < kParts; ++j)
-            v[u * 4 + i][j] = Word<kWide * kEs>::load(
-                rv, okv && z.v_at[j] != kNowhere ? z.v_at[j] + z.grp * 4 * token_bytes : kNowhere, i * token_bytes);
-        }
-      } else {
-        const u32 tk = t0 + z.col;
-        const bool seen = tk >= span.first && tk < span.end;
-        const u32 page = seen ? (u32)table[tk >> a.page_shift] : ~0u;
-        const bool ok = page < c.n_pages;
-        bad |= seen && !ok;
-        const uint8_t* p =
-            (const uint8_t*)c.k + (ok ? page * c.page_stride * kEs + (tk & (c.page_tokens - 1)) * (u64)token_bytes + head_bytes : 0);
+    for (int u = 0; u < 2; ++u) {
+      const u32 tk = t + u * 16 + z.col;
+      if (kSmall) {
+        const uint8_t* p = small(a, z, span, tk, a.d.kv.k, bad);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
           k[u][j] = 0;
-          if (ok && z.k_at[j] != kNowhere) k[u][j] = *(const v4u32*)(p + z.k_at[j]);
+          if (p && z.k_at[j] != kNowhere) k[u][j] = *(const v4u32*)(p + z.k_at[j]);
         }
+      } else {
+        const auto r = half(a, z, ids, u, t, a.d.kv.k);
+        const bool ok = ids.page[u] != ~0u && tk - span.first < span.end - span.first;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32 tv = t0 + z.grp * 4 + i;
-          const bool sv = tv >= span.first && tv < span.end;
-          const u32 pv = sv ? (u32)table[tv >> a.page_shift] : ~0u;
-          const bool okv = pv < c.n_pages;
-          const uint8_t* q =
-              (const uint8_t*)c.v + (okv ? pv * c.page_stride * kEs + (tv & (c.page_tokens - 1)) * (u64)token_bytes + head_bytes : 0);
+        for (int j = 0; j < kLoads; ++j) k[u][j] = Word<16>::load(r, ok ? z.k_at[j] : kNowhere, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void load_v(const Attend& a, const Lanes& z, const Span& span, const Ids& ids, u32 t, bool& bad) {
 #pragma unroll
-          for (int j = 0; j < kParts; ++j) {
+    for (int u = 0; u < 2; ++u) {
+      const auto r = kSmall ? buffer(nullptr, 0) : half(a, z, ids, u, t, a.d.kv.v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32 tv = t + u * 16 + z.grp * 4 + i;
+        const uint8_t* p = kSmall ? small(a, z, span, tv, a.d.kv.v, bad) : nullptr;
+        const bool ok = !kSmall && ids.page[u] != ~0u && tv - span.first < span.end - span.first;
+#pragma unroll
+        for (int j = 0; j < kParts; ++j) {
+          if (kSmall) {
             v[u * 4 + i][j] = 0;
-            if (okv && z.v_at[j] != kNowhere) v[u * 4 + i][j] = *(const vword*)(q + z.v_at[j]);
+            if (p && z.v_at[j] != kNowhere) v[u * 4 + i][j] = *(const vword*)(p + z.v_at[j]);
+          } else {
+            v[u * 4 + i][j] = Word<kWide * kEs>::load(r, ok ? z.v_at[j] : kNowhere, i * z.token_bytes);
           }
         }
       }
     }
   }
 
-  // Which of the lane's eight scores (tokens t + 16 u + 4 grp + i) have a key.
-  __device__ u32 seen(const Attend& a, const Lanes& z, const Span& span, u32 t) const {
-    u32 bits = 0;
-    const int* table = a.d.table + (u64)span.row * a.d.row_pages;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32 tok = t + u * 16 + z.grp * 4 + i;
-        bool ok = tok >= span.first && tok < span.end;
-        if (ok) ok = (u32)table[tok >> a.page_shift] < a.d.kv.n_pages;
-        bits |= (ok ? 1u : 0u) << (u * 4 + i);
-      }
-    return bits;
+  // Whether the lane's score i of half u (token t + 16 u + 4 grp + i) has a key.
+  __device__ __forceinline__ bool seen(const Attend& a, const Lanes& z, const Span& span, const Ids& ids, u32 t, int u, int i) const {
+    const u32 tok = t + u * 16 + z.grp * 4 + i;
+    const bool in = tok - span.first < span.end - span.first;
+    if (!kSmall) return in && ids.page[u] != ~0u;
+    return in && (u32)a.d.table[(u64)span.row * a.d.row_pages + (tok >> a.page_shift)] < a.d.kv.n_pages;
   }
 
   __device__ x8 key(int u, int step) const {
@@ -307,183 +358,251 @@ struct Tile {
 };
 
 // ---- the kernel -----------------------------------------------------------------------------------------
+// Workgroups of a compute unit that the registers leave room for.  (One more of 128 elements in 16 bits would leave 168, and
+// a few spills: their reloads wait behind all keys and values under way, and cost two thirds of the bandwidth.)
+constexpr u32 resident(int dim, bool f8) { return dim <= 64 ? 4 : dim <= 128 ? (f8 ? 3 : 2) : f8 ? 2 : 1; }
+
 template <typename T, bool kF8, int kDim, bool kSmall>
-__global__ void __launch_bounds__(256) attend_kernel(Attend a) {
+__global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend a) {
   typedef Tile<T, kF8, kDim, kSmall> Tl;
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
   constexpr int kWide = Tl::kWide, kParts = Tl::kParts, kSteps = Tl::kSteps, kPad = kDim + 4;
   __shared__ alignas(16) float s_o[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ u64 s_share[6];
   __shared__ u32 s_last;
 
   const u32 column = blockIdx.x % a.columns, at = blockIdx.x / a.columns;
-  const Piece piece = piece_of(a, uniform(at));
-  if (piece.none) return;
-  const u32 wave = threadIdx.x >> 6, seq = uniform(piece.seq), head = column / a.q_tiles, tile = column % a.q_tiles;
-  Span span = span_of(a, seq);
-  span.first = uniform(span.first), span.end = uniform(span.end), span.row = uniform(span.row);
-  bool bad = span.bad && piece.split == 0;
-  const u32 D = a.d.kv.head_dim, q0 = tile * 16;
+  Share share;
+  if (!find_share(a, at, share, s_share)) return;
+  const u32 wave = threadIdx.x >> 6, head = column / a.q_tiles, q0 = column % a.q_tiles * 16;
+  const u32 D = a.d.kv.head_dim, quads = D / 4;
   const u32 rows = a.group - q0 < 16 ? a.group - q0 : 16;  // query heads of this tile
-
+  const float scale = a.d.scale * (kF8 && a.d.kv.k_scale ? a.d.kv.k_scale[head] : 1.f) * kLog2e;
+  const float v_scale = kF8 && a.d.kv.v_scale ? a.d.kv.v_scale[head] : 1.f;
+  const u64 part_size = part_floats(a.rows, D);
   typename Tl::Lanes z;
   Tl::lanes(a, head, z);
 
-  // the tile's queries as the products' second operand: the same elements a lane as its keys
-  x8 q[kSteps];
-  {
-    const elem* src = (const elem*)a.d.q + seq * a.d.q_seq + (head * a.group + q0 + z.col) * a.d.q_head;
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st) {
-      const u32 e = kF8 ? (st / 2) * 64 + z.grp * 16 + (st & 1) * 8 : st * 32 + z.grp * 8;
-      const v4u32 none = 0;
-      q[st] = __builtin_bit_cast(x8, none);
-      if (z.col < rows && e < D) q[st] = *(const x8*)(src + e);
-    }
-  }
-  const float scale = a.d.scale * (kF8 && a.d.kv.k_scale ? a.d.kv.k_scale[head] : 1.f) * kLog2e;
+  u64 next = share.start;
+  for (u32 seq = share.seq; next < share.end; ++seq) {
+    const u64 start = next + kEach;  // place of the row's first tile
+    Span span = span_of(a, seq);
+    span.first = uniform(span.first), span.end = uniform(span.end), span.row = uniform(span.row);
+    const u32 all = span.tiles();
+    bool bad = span.bad;
+    const u64 place0 = next;
+    next = start + all;
+    // the tiles of the row that lie in the share; a row of none is its who has the row's first place
+    const u64 lo = start > share.begin ? start : share.begin, hi = next < share.end ? next : share.end;
+    if (all ? lo >= hi : place0 < share.begin) continue;
+    const u32 tile0 = span.first / kTile, begin = tile0 + (u32)(lo - start), end = all ? tile0 + (u32)(hi - start) : begin;
+    const bool whole = !all || (lo == start && hi == next);
 
-  f32x4 o[kParts * kWide];
+    // the tile's queries as the products' second operand: the same elements a lane as its keys
+    x8 q[kSteps];
+    {
+      const elem* src = (const elem*)a.d.q + seq * a.d.q_seq + (head * a.group + q0 + z.col) * a.d.q_head;
 #pragma unroll
-  for (int i = 0; i < kParts * kWide; ++i) o[i] = 0;
-  float m = -INFINITY, sum = 0.f;
-
-  const u32 all = span.tiles(), tile0 = span.first / kTile;
-  const u32 begin = tile0 + (u32)((u64)all * piece.split / piece.n_splits);
-  const u32 end = tile0 + (u32)((u64)all * (piece.split + 1) / piece.n_splits);
-  for (u32 i = begin + wave; i < end; i += kWaves) {
-    const u32 t = uniform(i * kTile);
-    Tl x;
-    x.load(a, z, span, head, t, bad);
-    f32x4 s[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = 0;
-#pragma unroll
-      for (int st = 0; st < kSteps; ++st) s[u] = mfma<T>(x.key(u, st), q[st], s[u]);
-    }
-    const u32 seen = x.seen(a, z, span, t);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i2 = 0; i2 < 4; ++i2) {
-        s[u][i2] = seen >> (u * 4 + i2) & 1 ? s[u][i2] * scale : -INFINITY;
-        mx = fmaxf(mx, s[u][i2]);
+      for (int st = 0; st < kSteps; ++st) {
+        const u32 e = kF8 ? (st / 2) * 64 + z.grp * 16 + (st & 1) * 8 : st * 32 + z.grp * 8;
+        const v4u32 none = 0;
+        q[st] = __builtin_bit_cast(x8, none);
+        if (z.col < rows && e < D) q[st] = *(const x8*)(src + e);
       }
-    mx = over_groups(mx, larger);
-    const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-    const float keep = __builtin_amdgcn_exp2f(m - ref);
-    m = m_new;
-    x8 p;
-    float part = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float e = __builtin_amdgcn_exp2f(s[j / 4][j % 4] - ref);
-      part += e;
-      p[j] = (elem)e;
     }
-    sum = sum * keep + part;
+
+    f32x4 o[kParts * kWide];
+#pragma unroll
+    for (int i = 0; i < kParts * kWide; ++i) o[i] = 0;
+    float m = -INFINITY, sum = 0.f;
+
+    // keys of the next tile are asked for as soon as this one's are used up, values likewise: there is always as much under
+    // way as the registers hold
+    const u32 t_end = end * kTile;
+    u32 t = uniform((begin + wave) * kTile);
+    if (t < t_end) {
+      Tl x;
+      typename Tl::Ids ids = Tl::ids(a, span, t, bad);
+      x.load_k(a, z, span, ids, t, bad);
+      x.load_v(a, z, span, ids, t, bad);
+      for (; t < t_end; t += kWaves * kTile) {
+        const u32 t_next = t + kWaves * kTile < t_end ? t + kWaves * kTile : 0x7fffffc0u;  // behind every row
+        const typename Tl::Ids ids_next = Tl::ids(a, span, t_next, bad);
+        f32x4 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[u] = 0;
+#pragma unroll
+          for (int st = 0; st < kSteps; ++st) s[u] = mfma<T>(x.key(u, st), q[st], s[u]);
+        }
+        x.load_k(a, z, span, ids_next, t_next, bad);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[u][i] = x.seen(a, z, span, ids, t, u, i) ? s[u][i] * scale : -INFINITY;
+            mx = fmaxf(mx, s[u][i]);
+          }
+        mx = over_groups(mx, larger);
+        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float keep = __builtin_amdgcn_exp2f(m - ref);
+        m = m_new;
+        x8 p;
+        float part = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float e = __builtin_amdgcn_exp2f(s[j / 4][j % 4] - ref);
+          part += e;
+          p[j] = (elem)e;
+        }
+        sum = sum * keep + part;
+#pragma unroll
+        for (int part_ = 0; part_ < kParts; ++part_)
+#pragma unroll
+          for (int e2 = 0; e2 < kWide / 2; ++e2) {
+            v4u32 low, high;  // eight tokens of elements 2 e2 and 2 e2 + 1
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const u32 x0 = x.value2(2 * j, part_, e2), x1 = x.value2(2 * j + 1, part_, e2);
+              low[j] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+              high[j] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+            }
+            f32x4& c0 = o[part_ * kWide + 2 * e2];
+            f32x4& c1 = o[part_ * kWide + 2 * e2 + 1];
+            c0 = mfma<T>(__builtin_bit_cast(x8, low), p, c0 * keep);
+            c1 = mfma<T>(__builtin_bit_cast(x8, high), p, c1 * keep);
+          }
+        x.load_v(a, z, span, ids_next, t_next, bad);
+        ids = ids_next;
+      }
+    }
+    sum = over_groups(sum, plus);
+    if (ballot(bad) && lane_id() == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
+
+    // the four waves' sums, joined
 #pragma unroll
     for (int part_ = 0; part_ < kParts; ++part_)
 #pragma unroll
-      for (int e2 = 0; e2 < kWide / 2; ++e2) {
-        v4u32 lo, hi;  // eight tokens of elements 2 e2 and 2 e2 + 1
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32 x0 = x.value2(2 * j, part_, e2), x1 = x.value2(2 * j + 1, part_, e2);
-          lo[j] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-          hi[j] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-        }
-        f32x4& c0 = o[part_ * kWide + 2 * e2];
-        f32x4& c1 = o[part_ * kWide + 2 * e2 + 1];
-        c0 = mfma<T>(__builtin_bit_cast(x8, lo), p, c0 * keep);
-        c1 = mfma<T>(__builtin_bit_cast(x8, hi), p, c1 * keep);
+        for (int e = 0; e < kWide; ++e)
+          s_o[wave][z.col][part_ * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[part_ * kWide + e][i];
+    if (z.grp == 0) s_m[wave][z.col] = m, s_l[wave][z.col] = sum;
+    __syncthreads();
+    const auto mine = part_buffer(a.parts + (((u64)at * a.columns + column) * 2 + (start > share.begin)) * part_size, part_size);
+    auto finish = [&](u32 r, u32 qd, float M, float L, f32x4 x) {
+      const u32 h = head * a.group + q0 + r;
+      x = x * (L == 0.f ? 0.f : v_scale / L);
+      elem* out = (elem*)a.d.out + seq * a.d.out_seq + h * a.d.out_head + qd * 4;
+      typedef elem x4 __attribute__((ext_vector_type(4)));
+      *(x4*)out = __builtin_convertvector(x, x4);
+      if (qd == 0 && a.d.lse) a.d.lse[(u64)seq * a.d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
+    };
+    for (u32 i = threadIdx.x; i < rows * quads; i += 256) {
+      const u32 r = i / quads, qd = i - r * quads;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < (int)kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+      const float ref = M == -INFINITY ? 0.f : M;
+      float L = 0.f;
+      f32x4 x = 0;
+#pragma unroll
+      for (int w = 0; w < (int)kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
+        L += f * s_l[w][r];
+        x += f * *(const f32x4*)&s_o[w][r][qd * 4];
       }
-  }
-  sum = over_groups(sum, plus);
-  if (ballot(bad) && lane_id() == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
+      if (whole) {
+        finish(r, qd, ref, L, x);
+      } else {
+        put_part(mine, r * D + qd * 4, x);
+        if (qd == 0) put_part(mine, a.rows * D + 2 * r, M, L);
+      }
+    }
+    if (whole) {
+      __syncthreads();  // the next row's sums go where these lay
+      continue;
+    }
 
-  // the four waves' sums, joined
-#pragma unroll
-  for (int part_ = 0; part_ < kParts; ++part_)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < kWide; ++e) s_o[wave][z.col][part_ * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[part_ * kWide + e][i];
-  if (z.grp == 0) s_m[wave][z.col] = m, s_l[wave][z.col] = sum;
-  __syncthreads();
-  const u32 quads = D / 4;
-  const float v_scale = kF8 && a.d.kv.v_scale ? a.d.kv.v_scale[head] : 1.f;
-  const u64 slot_floats = part_floats(a.rows, D);
-  float* mine = a.parts + ((u64)piece.at * a.columns + column) * slot_floats;
-  auto finish = [&](u32 r, u32 qd, float M, float L, f32x4 x) {
-    const u32 h = head * a.group + q0 + r;
-    x = x * (L == 0.f ? 0.f : v_scale / L);
-    elem* out = (elem*)a.d.out + seq * a.d.out_seq + h * a.d.out_head + qd * 4;
-    typedef elem x4 __attribute__((ext_vector_type(4)));
-    *(x4*)out = __builtin_convertvector(x, x4);
-    if (qd == 0 && a.d.lse) a.d.lse[(u64)seq * a.d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
-  };
-  for (u32 i = threadIdx.x; i < rows * quads; i += 256) {
-    const u32 r = i / quads, qd = i - r * quads;
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < (int)kWaves; ++w) M = fmaxf(M, s_m[w][r]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
-    f32x4 x = 0;
-#pragma unroll
-    for (int w = 0; w < (int)kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
-      L += f * s_l[w][r];
-      x += f * *(const f32x4*)&s_o[w][r][qd * 4];
+    // the row's parts, joined by the workgroup that finishes last; its counter is left at zero
+    const u32 first = (u32)(start / share.per), n_parts = (u32)((next - 1) / share.per) - first + 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has arrived where all workgroups see it
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      u32* counter = a.counters + seq * a.columns + column;
+      const u32 before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      s_last = before == n_parts - 1;
+      if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (piece.n_splits == 1) {
-      finish(r, qd, ref, L, x);
-    } else {
-      *(f32x4*)(mine + r * D + qd * 4) = x;
-      if (qd == 0) mine[a.rows * D + r] = M, mine[a.rows * (D + 1) + r] = L;
+    __syncthreads();
+    if (!s_last) continue;  // (s_last is written again only behind the next row's barriers)
+    // the first part is the second of its share, unless the share begins with the row
+    auto part = [&](u32 k) {
+      const u32 second = k == 0 && start > first * share.per;
+      return part_buffer(a.parts + ((((u64)first + k) * a.columns + column) * 2 + second) * part_size, part_size);
+    };
+    // `crews` of threads take every crews-th part each, eight parts' loads under way
+    const u32 items = rows * quads, crews = items >= 256 ? 1 : 256 / items;
+    for (u32 i0 = 0; i0 < items; i0 += 256) {
+      const u32 i = i0 + (crews > 1 ? threadIdx.x % items : threadIdx.x), crew = crews > 1 ? threadIdx.x / items : 0;
+      const u32 r = i / quads, qd = i - r * quads;
+      const bool works = i < items && crew < crews;
+      float M = -INFINITY, L = 0.f;
+      f32x4 x = 0;
+      if (works) {
+        for (u32 k0 = crew; k0 < n_parts; k0 += crews * 8) {
+          f32x4 y[8];
+          v2u32 ml[8];
+#pragma unroll
+          for (u32 j = 0; j < 8; ++j) {
+            const u32 k = k0 + j * crews < n_parts ? k0 + j * crews : k0;
+            y[j] = get_part4(part(k), r * D + qd * 4);
+            ml[j] = get_part2(part(k), a.rows * D + 2 * r);
+          }
+          float top = M;
+#pragma unroll
+          for (u32 j = 0; j < 8; ++j) top = fmaxf(top, as_float(ml[j].x));
+          const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(M - ref);
+          x *= keep, L *= keep, M = top;
+#pragma unroll
+          for (u32 j = 0; j < 8; ++j)
+            if (k0 + j * crews < n_parts) {
+              const float f = __builtin_amdgcn_exp2f(as_float(ml[j].x) - ref);
+              L += f * as_float(ml[j].y);
+              x += f * y[j];
+            }
+        }
+      }
+      if (crews > 1) {  // the crews' sums, in their order
+        float(*c_x)[4] = (float(*)[4])s_o;
+        float(*c_ml)[2] = (float(*)[2])(c_x + 256);
+        if (works) *(f32x4*)c_x[threadIdx.x] = x, c_ml[threadIdx.x][0] = M, c_ml[threadIdx.x][1] = L;
+        __syncthreads();
+        if (works && crew == 0) {
+          float top = M;
+          for (u32 c = 1; c < crews; ++c) top = fmaxf(top, c_ml[c * items + i][0]);
+          const float ref = top == -INFINITY ? 0.f : top;
+          float f = __builtin_amdgcn_exp2f(M - ref);
+          x *= f, L *= f, M = top;
+          for (u32 c = 1; c < crews; ++c) {
+            f = __builtin_amdgcn_exp2f(c_ml[c * items + i][0] - ref);
+            L += f * c_ml[c * items + i][1];
+            x += f * *(const f32x4*)c_x[c * items + i];
+          }
+        }
+      }
+      if (works && crew == 0) finish(r, qd, M == -INFINITY ? 0.f : M, L, x);
     }
-  }
-  if (piece.n_splits == 1) return;
-
-  // the row's pieces, joined by the workgroup that finishes last; its counter is left at zero
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    u32* counter = a.counters + seq * a.columns + column;
-    const u32 before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = before == piece.n_splits - 1;
-    if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-  const float* parts = a.parts + ((u64)(piece.at - piece.split) * a.columns + column) * slot_floats;
-  const u64 apart = (u64)a.columns * slot_floats;
-  for (u32 i = threadIdx.x; i < rows * quads; i += 256) {
-    const u32 r = i / quads, qd = i - r * quads;
-    float M = -INFINITY;
-    for (u32 k = 0; k < piece.n_splits; ++k) M = fmaxf(M, parts[k * apart + a.rows * D + r]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
-    f32x4 x = 0;
-#pragma unroll 4
-    for (u32 k = 0; k < piece.n_splits; ++k) {
-      const float* p = parts + k * apart;
-      const float f = __builtin_amdgcn_exp2f(p[a.rows * D + r] - ref);
-      L += f * p[a.rows * (D + 1) + r];
-      x += f * *(const f32x4*)(p + r * D + qd * 4);
-    }
-    finish(r, qd, ref, L, x);
+    __syncthreads();  // the next row's sums go where the crews' lay
   }
 }
 
 template <typename T, bool kF8, int kDim>
 int launch_attend(const Attend& a, hipStream_t stream) {
-  const u32 blocks = (a.d.n_seqs + a.extra) * a.columns;
+  const u32 blocks = a.shares * a.columns;
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
   if (a.d.kv.page_tokens < 16)
     hipLaunchKernelGGL((attend_kernel<T, kF8, kDim, true>), dim3(blocks), dim3(256), 0, stream, a);
@@ -516,10 +635,12 @@ void lay_out(const fdy_attend& d, Attend& a) {
   a.q_tiles = (a.group + 15) / 16;
   a.columns = d.kv.n_heads * a.q_tiles;
   a.rows = a.group < 16 ? a.group : 16;
-  // pieces beyond one a row: enough to fill the chip with four workgroups a compute unit, and to halve rows longer than
-  // the mean where there are more rows than that
-  a.extra = (kCus * 4 + a.columns - 1) / a.columns;
-  if (a.extra < d.n_seqs) a.extra = d.n_seqs;
+  // as many workgroups as are resident together, fewer where the longest rows that the table allows have not the tiles
+  a.shares = kCus * resident((int)d.kv.head_dim, d.kv.type == FDY_F8) / a.columns;
+  if (a.shares < 1) a.shares = 1;
+  const u64 places = (u64)d.n_seqs * ((((u64)d.row_pages << a.page_shift) + kTile - 1) / kTile + 1 + kEach);
+  const u64 most = (places + kLeast + kEach - 1) / (kLeast + kEach);
+  if (a.shares > most) a.shares = most < 1 ? 1 : (u32)most;
 }
 size_t counter_bytes(const Attend& a) { return ((size_t)a.d.n_seqs * a.columns * 4 + 255) / 256 * 256; }
 
@@ -529,7 +650,7 @@ extern "C" size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h) {
   if (!h || !sizes_valid(*h)) return 0;
   Attend a{};
   lay_out(*h, a);
-  const size_t parts = (size_t)(h->n_seqs + a.extra) * a.columns * part_floats(a.rows, h->kv.head_dim) * 4;
+  const size_t parts = (size_t)a.shares * a.columns * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
   return counter_bytes(a) + (parts + 255) / 256 * 256;
 }
 
