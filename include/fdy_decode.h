@@ -143,7 +143,7 @@ int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stre
  * time for the same call.
  *   q, out, kv.k, kv.v 16-byte aligned, strides multiples of 8 elements (kv's of 16 bytes); head_dim a multiple of 8
  *   (of 16 with F8) up to 256; n_q_heads a multiple of kv.n_heads; kv.type is `type` or FDY_F8; n_seqs <= 65,536,
- *   n_q_heads <= 65,536, n_seqs * n_q_heads <= 2^22, row_pages * page_tokens < 2^31.
+ *   n_q_heads <= 65,536, n_seqs * n_q_heads <= 2^22, row_pages * page_tokens < 2^31, n_seqs times that <= 2^36.
  *   workspace  device, 256-byte aligned, fdy_paged_attention_workspace_bytes() (0: a field out of range).  The caller
  *              clears it once, before its first use; every call leaves what it needs cleared cleared.  Calls that share one
  *              must not overlap in time, and after FDY_ERR_HIP it is cleared again.  One sized for a descriptor serves

@@ -21,8 +21,8 @@ using namespace fdy;
 namespace {
 
 constexpr u32 kWaves = 4, kTile = 32, kCus = 256;
-constexpr u32 kLeast = 8;  // tiles of a share, at least: two for each wave
-constexpr u32 kEach = 4;   // what a row costs beside its tiles (queries, join, output), in tiles
+constexpr u32 kLeast = 4;  // tiles of a share, at least: one for each wave
+constexpr u32 kEach = 3;   // what a row costs beside its tiles (queries, join, output), in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArg {
@@ -30,7 +30,8 @@ struct AttendArg {
   u32* status;
   u32* counters;  // [n_seqs][columns], zero between calls
   float* parts;   // [shares][columns][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
-  u32 page_shift, group, q_tiles, columns, shares, rows;  // columns: cache heads x q_tiles; rows: query heads of a tile
+  // columns: cache heads x q_tiles; rows: query heads of a tile; together: columns that a workgroup may take at once
+  u32 page_shift, group, q_tiles, columns, rows, together;
 };
 typedef Arg<AttendArg> Attend;
 
@@ -82,7 +83,6 @@ __device__ __forceinline__ float plus(float a, float b) { return a + b; }
 // Parts go from one workgroup to another, on another die as it may be: they are written through to memory and read from
 // there (device scope on each access), for a fence would write back and drop all that the dies' caches hold, once a wave.
 constexpr int kDeviceScope = 0x10;  // sc1
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t part_buffer(float* part, u64 floats) { return buffer(part, (u32)floats * 4); }
 __device__ __forceinline__ float as_float(u32 v) { return __builtin_bit_cast(float, v); }
 __device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t part, u32 at, f32x4 x) {
   __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u32, x), part, at * 4, 0, kDeviceScope);
@@ -125,80 +125,86 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 s) {
 // The rows' tiles lie one after the other on a line, kEach places ahead of each row's; equal shares of the line go to the
 // workgroups of a column.  So all of them have the same to do whatever the lengths are, and a row is in as many parts as
 // shares reach into it.
+//
+// A workgroup takes one column, its four waves every fourth tile, or `together` of them, as many waves as that leaves to each:
+// where the heads of a token lie side by side, one head's keys are 128 or 256 bytes at every n_heads-th place, and memory
+// gives less of them than of the four heads' as one piece (TB/s, 4,096 tokens a row, 8 heads: 128 rows in 8 bits 4.8 alone,
+// 64 rows in 16 bits 5.8).  It takes enough tiles that a wave has kFew of them to itself.
 struct Share {
-  u64 begin, end, per;  // places
-  u32 seq;              // row at `begin`, and where it starts
-  u64 start;
+  u32 begin, end, per;  // places
+  u32 seq, start;       // the row at `begin`, and its own place
+  u32 at, column, together;
 };
+constexpr u32 kFew = 16;
 
-__device__ __forceinline__ u64 share_of(const Attend& a, u64 total) {
-  const u64 per = (total + a.shares - 1) / a.shares;
-  return per < kLeast + kEach ? kLeast + kEach : per;
-}
-
-// All threads of the workgroup; s_share: 6 u64 of LDS.
-__device__ __forceinline__ bool find_share(const Attend& a, u32 at, Share& out, u64* s_share) {
-  const u32 n = a.d.n_seqs, tid = threadIdx.x;
+// All threads of the workgroup; s_share: 6 words of LDS.
+__device__ __forceinline__ bool find_share(const Attend& a, Share& out, u32* s_share) {
+  const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + 255) / 256;
+  const u32 s0 = tid * slice, s1 = s0 + slice < n ? s0 + slice : n;
+  u32 mine = 0, before = 0, total = 0;
   if (n == 1) {
-    const u64 total = span_of(a, 0).tiles() + kEach;
-    out.per = share_of(a, total);
-    out.begin = at * out.per;
-    out.end = out.begin + out.per < total ? out.begin + out.per : total;
-    out.seq = 0, out.start = 0;
-    return out.begin < total;
-  }
-  const u32 slice = (n + 255) / 256, s0 = tid * slice, s1 = s0 + slice < n ? s0 + slice : n;
-  u64 mine = 0;
-  for (u32 s = s0; s < s1; ++s) mine += span_of(a, s).tiles() + kEach;
-  const u64 inc = wave_incl_scan(mine);
-  if (lane_id() == 63) s_share[tid >> 6] = inc;
-  __syncthreads();
-  u64 before = inc - mine, total = 0;
+    total = span_of(a, 0).tiles() + kEach;
+  } else {
+    for (u32 s = s0; s < s1; ++s) mine += span_of(a, s).tiles() + kEach;
+    const u32 inc = wave_incl_scan(mine);
+    if (lane_id() == 63) s_share[tid >> 6] = inc;
+    __syncthreads();
+    before = inc - mine;
 #pragma unroll
-  for (u32 w = 0; w < kWaves; ++w) {
-    if (w < tid >> 6) before += s_share[w];
-    total += s_share[w];
+    for (u32 w = 0; w < kWaves; ++w) {
+      if (w < tid >> 6) before += s_share[w];
+      total += s_share[w];
+    }
   }
-  out.per = share_of(a, total);
-  out.begin = at * out.per;
-  out.end = out.begin + out.per < total ? out.begin + out.per : total;
-  if (out.begin >= total) return false;
+  total = uniform(total);
+  out.together = (u64)total * a.columns >= (u64)gridDim.x * kWaves * kFew ? a.together : 1;
+  const u32 columns = a.columns / out.together, shares = gridDim.x / columns, least = kLeast + kEach;
+  out.at = blockIdx.x / columns, out.column = blockIdx.x % columns * out.together;
+  out.per = (total - 1) / shares + 1;
+  if (out.per < least) out.per = least;
+  if (out.at >= shares || (u64)out.at * out.per >= total) return false;
+  out.begin = out.at * out.per;
+  out.end = total - out.begin > out.per ? out.begin + out.per : total;
+  out.seq = 0, out.start = 0;
+  if (n == 1) return true;
   if (out.begin >= before && out.begin < before + mine) {
     u32 s = s0;
     for (;; ++s) {
-      const u64 cost = span_of(a, s).tiles() + kEach;
+      const u32 cost = span_of(a, s).tiles() + kEach;
       if (out.begin < before + cost) break;
       before += cost;
     }
     s_share[4] = s, s_share[5] = before;
   }
   __syncthreads();
-  out.seq = uniform((u32)s_share[4]), out.start = uniform(s_share[5]);
+  out.seq = uniform(s_share[4]), out.start = uniform(s_share[5]);
   return true;
 }
 
 // ---- loads ------------------------------------------------------------------------------------------
-template <int kBytes>
+// Keys and values that are read once are marked so (two rows of 10^5 tokens: 171 us, marked 154); those of more than 16 query
+// heads of a cache head are read once for each 16, and not (32 of one: 77 us, marked 95).
+template <int kBytes, int kPolicy>
 struct Word;
-template <>
-struct Word<16> {
+template <int kPolicy>
+struct Word<16, kPolicy> {
   typedef v4u32 type;
   static __device__ type load(__amdgpu_buffer_rsrc_t r, u32 at, u32 plus) {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, at, plus, 0);
+    return __builtin_amdgcn_raw_buffer_load_b128(r, at, plus, kPolicy);
   }
 };
-template <>
-struct Word<8> {
+template <int kPolicy>
+struct Word<8, kPolicy> {
   typedef v2u32 type;
   static __device__ type load(__amdgpu_buffer_rsrc_t r, u32 at, u32 plus) {
-    return __builtin_amdgcn_raw_buffer_load_b64(r, at, plus, 0);
+    return __builtin_amdgcn_raw_buffer_load_b64(r, at, plus, kPolicy);
   }
 };
-template <>
-struct Word<4> {
+template <int kPolicy>
+struct Word<4, kPolicy> {
   typedef u32 type;
   static __device__ type load(__amdgpu_buffer_rsrc_t r, u32 at, u32 plus) {
-    return __builtin_amdgcn_raw_buffer_load_b32(r, at, plus, 0);
+    return __builtin_amdgcn_raw_buffer_load_b32(r, at, plus, kPolicy);
   }
 };
 
@@ -213,7 +219,7 @@ __device__ __forceinline__ u32 word<u32>(const u32& w, int) {
 
 // kDim: head_dim rounded up to 64, 128 or 256.  kSmall: pages of less than 16 tokens, where 16 tokens lie in several pages
 // and every lane looks its own up; otherwise 16 tokens have one page, whose address is the wave's.
-template <typename T, bool kF8, int kDim, bool kSmall>
+template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy>
 struct Tile {
   typedef typename T::x8 x8;
   static constexpr int kEs = kF8 ? 1 : 2;
@@ -221,7 +227,7 @@ struct Tile {
   static constexpr int kSteps = kDim / 32;                // products over 32 elements
   static constexpr int kWide = kDim >= 128 ? 8 : kDim / 16;  // elements of v a lane and token
   static constexpr int kParts = kDim / (16 * kWide);      // of v's row
-  typedef typename Word<kWide * kEs>::type vword;
+  typedef typename Word<kWide * kEs, kPolicy>::type vword;
   v4u32 k[2][kLoads];
   vword v[8][kParts];
 
@@ -308,7 +314,7 @@ struct Tile {
         const auto r = half(a, z, ids, u, t, a.d.kv.k);
         const bool ok = ids.page[u] != ~0u && tk - span.first < span.end - span.first;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) k[u][j] = Word<16>::load(r, ok ? z.k_at[j] : kNowhere, 0);
+        for (int j = 0; j < kLoads; ++j) k[u][j] = Word<16, kPolicy>::load(r, ok ? z.k_at[j] : kNowhere, 0);
       }
     }
   }
@@ -327,7 +333,7 @@ struct Tile {
             v[u * 4 + i][j] = 0;
             if (p && z.v_at[j] != kNowhere) v[u * 4 + i][j] = *(const vword*)(p + z.v_at[j]);
           } else {
-            v[u * 4 + i][j] = Word<kWide * kEs>::load(r, ok ? z.v_at[j] : kNowhere, i * z.token_bytes);
+            v[u * 4 + i][j] = Word<kWide * kEs, kPolicy>::load(r, ok ? z.v_at[j] : kNowhere, i * z.token_bytes);
           }
         }
       }
@@ -349,55 +355,68 @@ struct Tile {
     return __builtin_bit_cast(x8, w);
   }
 
-  // Elements 2 e, 2 e + 1 of the lane's piece of a token's v.
-  __device__ u32 value2(int token, int part, int e) const {
-    if (!kF8) return word(v[token][part], e);
-    const u32 w = word(v[token][part], e / 2);
-    return e & 1 ? widen_f8x2<T, true>(w) : widen_f8x2<T, false>(w);
+  // Elements 2 e and 2 e + 1 of the lane's piece of v, of its eight tokens: the products' first operand.
+  __device__ __forceinline__ void values(int part, int e, x8& even, x8& odd) const {
+    v4u32 lo, hi;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (kF8) {  // bytes {x, y, x', y'} of tokens 2 j and 2 j + 1, widened two at a time
+        const u32 x = word(v[2 * j][part], e / 2), y = word(v[2 * j + 1][part], e / 2);
+        const u32 xy = __builtin_amdgcn_perm(y, x, e & 1 ? 0x07030602u : 0x05010400u);
+        lo[j] = widen_f8x2<T, false>(xy), hi[j] = widen_f8x2<T, true>(xy);
+      } else {
+        const u32 x = word(v[2 * j][part], e), y = word(v[2 * j + 1][part], e);
+        lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u), hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+      }
+    }
+    even = __builtin_bit_cast(x8, lo), odd = __builtin_bit_cast(x8, hi);
   }
 };
 
 // ---- the kernel -----------------------------------------------------------------------------------------
-// Workgroups of a compute unit that the registers leave room for.  (One more of 128 elements in 16 bits would leave 168, and
-// a few spills: their reloads wait behind all keys and values under way, and cost two thirds of the bandwidth.)
-constexpr u32 resident(int dim, bool f8) { return dim <= 64 ? 4 : dim <= 128 ? (f8 ? 3 : 2) : f8 ? 2 : 1; }
+// Workgroups of a compute unit that are launched, and that the registers leave room for.  More do not help: of rows of 4,096
+// tokens in 8 bits, three give 4.6 TB/s where two give 5.1; and one more of 128 elements in 16 bits leaves 168 registers and
+// a few spills, whose reloads wait behind all keys and values under way (2.1 TB/s).
+constexpr u32 resident(int dim) { return dim <= 128 ? 2 : 1; }
 
-template <typename T, bool kF8, int kDim, bool kSmall>
-__global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend a) {
-  typedef Tile<T, kF8, kDim, kSmall> Tl;
+template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy>
+__global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
+  typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
   constexpr int kWide = Tl::kWide, kParts = Tl::kParts, kSteps = Tl::kSteps, kPad = kDim + 4;
   __shared__ alignas(16) float s_o[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  __shared__ u64 s_share[6];
+  __shared__ u32 s_share[6];
   __shared__ u32 s_last;
 
-  const u32 column = blockIdx.x % a.columns, at = blockIdx.x / a.columns;
   Share share;
-  if (!find_share(a, at, share, s_share)) return;
-  const u32 wave = threadIdx.x >> 6, head = column / a.q_tiles, q0 = column % a.q_tiles * 16;
-  const u32 D = a.d.kv.head_dim, quads = D / 4;
-  const u32 rows = a.group - q0 < 16 ? a.group - q0 : 16;  // query heads of this tile
-  const float scale = a.d.scale * (kF8 && a.d.kv.k_scale ? a.d.kv.k_scale[head] : 1.f) * kLog2e;
-  const float v_scale = kF8 && a.d.kv.v_scale ? a.d.kv.v_scale[head] : 1.f;
-  const u64 part_size = part_floats(a.rows, D);
+  if (!find_share(a, share, s_share)) return;
+  const u32 together = share.together, apart = kWaves / together;  // `apart`: waves of a column
+  const u32 wave = threadIdx.x >> 6, turn = uniform(wave / together), column = uniform(share.column + wave % together);
+  const u32 head = column / a.q_tiles, q0 = column % a.q_tiles * 16;
+  const u32 D = a.d.kv.head_dim, quads = D / 4, part_size = part_floats(a.rows, D);
+  const auto parts = buffer(a.parts, gridDim.x * a.together * 2 * part_size * 4);  // within 2^30 bytes
+  // the factor of the scores, made positive (its sign goes to the queries; where it is 0 they are 0, too), so that the largest
+  // score is the one of the largest product and masked ones stay minus infinity
+  const float factor = a.d.scale * (kF8 && a.d.kv.k_scale ? a.d.kv.k_scale[head] : 1.f) * kLog2e;
+  const float scale = factor == 0.f ? 1.f : fabsf(factor);
+  const u32 q_keep = factor == 0.f ? 0u : ~0u, q_flip = factor < 0.f ? 0x80008000u : 0u;
   typename Tl::Lanes z;
   Tl::lanes(a, head, z);
 
-  u64 next = share.start;
+  u32 next = share.start;
   for (u32 seq = share.seq; next < share.end; ++seq) {
-    const u64 start = next + kEach;  // place of the row's first tile
+    const u32 first_place = next, start = next + kEach;  // places of the row, and of its first tile
     Span span = span_of(a, seq);
     span.first = uniform(span.first), span.end = uniform(span.end), span.row = uniform(span.row);
     const u32 all = span.tiles();
     bool bad = span.bad;
-    const u64 place0 = next;
     next = start + all;
     // the tiles of the row that lie in the share; a row of none is its who has the row's first place
-    const u64 lo = start > share.begin ? start : share.begin, hi = next < share.end ? next : share.end;
-    if (all ? lo >= hi : place0 < share.begin) continue;
-    const u32 tile0 = span.first / kTile, begin = tile0 + (u32)(lo - start), end = all ? tile0 + (u32)(hi - start) : begin;
+    const u32 lo = start > share.begin ? start : share.begin, hi = next < share.end ? next : share.end;
+    if (all ? lo >= hi : first_place < share.begin) continue;
+    const u32 tile0 = span.first / kTile, begin = tile0 + lo - start, end = all ? tile0 + hi - start : begin;
     const bool whole = !all || (lo == start && hi == next);
 
     // the tile's queries as the products' second operand: the same elements a lane as its keys
@@ -407,9 +426,9 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
         const u32 e = kF8 ? (st / 2) * 64 + z.grp * 16 + (st & 1) * 8 : st * 32 + z.grp * 8;
-        const v4u32 none = 0;
-        q[st] = __builtin_bit_cast(x8, none);
-        if (z.col < rows && e < D) q[st] = *(const x8*)(src + e);
+        v4u32 w = 0;
+        if (q0 + z.col < a.group && z.col < 16 && e < D) w = *(const v4u32*)(src + e);
+        q[st] = __builtin_bit_cast(x8, (w & q_keep) ^ q_flip);
       }
     }
 
@@ -420,15 +439,15 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
 
     // keys of the next tile are asked for as soon as this one's are used up, values likewise: there is always as much under
     // way as the registers hold
-    const u32 t_end = end * kTile;
-    u32 t = uniform((begin + wave) * kTile);
+    const u32 t_end = end * kTile, t_step = apart * kTile;
+    u32 t = uniform((begin + turn) * kTile);
     if (t < t_end) {
       Tl x;
       typename Tl::Ids ids = Tl::ids(a, span, t, bad);
       x.load_k(a, z, span, ids, t, bad);
       x.load_v(a, z, span, ids, t, bad);
-      for (; t < t_end; t += kWaves * kTile) {
-        const u32 t_next = t + kWaves * kTile < t_end ? t + kWaves * kTile : 0x7fffffc0u;  // behind every row
+      for (; t < t_end; t += t_step) {
+        const u32 t_next = t + t_step < t_end ? t + t_step : 0x7fffffc0u;  // behind every row
         const typename Tl::Ids ids_next = Tl::ids(a, span, t_next, bad);
         f32x4 s[2];
 #pragma unroll
@@ -438,15 +457,13 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
           for (int st = 0; st < kSteps; ++st) s[u] = mfma<T>(x.key(u, st), q[st], s[u]);
         }
         x.load_k(a, z, span, ids_next, t_next, bad);
-        float mx = -INFINITY;
+        float y[8];  // the lane's products, those without a key at minus infinity
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int j = 0; j < 8; ++j) y[j] = x.seen(a, z, span, ids, t, j / 4, j % 4) ? s[j / 4][j % 4] : -INFINITY;
+        float mx = y[0];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[u][i] = x.seen(a, z, span, ids, t, u, i) ? s[u][i] * scale : -INFINITY;
-            mx = fmaxf(mx, s[u][i]);
-          }
-        mx = over_groups(mx, larger);
+        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, y[j]);
+        mx = over_groups(mx, larger) * scale;
         const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
         const float keep = __builtin_amdgcn_exp2f(m - ref);
         m = m_new;
@@ -454,26 +471,21 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
         float part = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float e = __builtin_amdgcn_exp2f(s[j / 4][j % 4] - ref);
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], scale, -ref));
           part += e;
           p[j] = (elem)e;
         }
         sum = sum * keep + part;
 #pragma unroll
-        for (int part_ = 0; part_ < kParts; ++part_)
+        for (int pt = 0; pt < kParts; ++pt)
 #pragma unroll
           for (int e2 = 0; e2 < kWide / 2; ++e2) {
-            v4u32 low, high;  // eight tokens of elements 2 e2 and 2 e2 + 1
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const u32 x0 = x.value2(2 * j, part_, e2), x1 = x.value2(2 * j + 1, part_, e2);
-              low[j] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-              high[j] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-            }
-            f32x4& c0 = o[part_ * kWide + 2 * e2];
-            f32x4& c1 = o[part_ * kWide + 2 * e2 + 1];
-            c0 = mfma<T>(__builtin_bit_cast(x8, low), p, c0 * keep);
-            c1 = mfma<T>(__builtin_bit_cast(x8, high), p, c1 * keep);
+            x8 even, odd;
+            x.values(pt, e2, even, odd);
+            f32x4& c0 = o[pt * kWide + 2 * e2];
+            f32x4& c1 = o[pt * kWide + 2 * e2 + 1];
+            c0 = mfma<T>(even, p, c0 * keep);
+            c1 = mfma<T>(odd, p, c1 * keep);
           }
         x.load_v(a, z, span, ids_next, t_next, bad);
         ids = ids_next;
@@ -482,44 +494,61 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
     sum = over_groups(sum, plus);
     if (ballot(bad) && lane_id() == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
 
-    // the four waves' sums, joined
+    // the waves' sums, joined
 #pragma unroll
-    for (int part_ = 0; part_ < kParts; ++part_)
+    for (int pt = 0; pt < kParts; ++pt)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int e = 0; e < kWide; ++e)
-          s_o[wave][z.col][part_ * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[part_ * kWide + e][i];
+        for (int e = 0; e < kWide; ++e) s_o[wave][z.col][pt * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[pt * kWide + e][i];
     if (z.grp == 0) s_m[wave][z.col] = m, s_l[wave][z.col] = sum;
     __syncthreads();
-    const auto mine = part_buffer(a.parts + (((u64)at * a.columns + column) * 2 + (start > share.begin)) * part_size, part_size);
-    auto finish = [&](u32 r, u32 qd, float M, float L, f32x4 x) {
-      const u32 h = head * a.group + q0 + r;
+    // item i: four elements (from 4 qd on) of query head r of column c of the workgroup's
+    struct Item {
+      u32 c, r, qd;
+      bool there;
+    };
+    const u32 items = together * a.rows * quads;
+    auto item = [&](u32 i) {
+      Item it;
+      const u32 row = i / quads;
+      it.qd = i - row * quads, it.c = row / a.rows, it.r = row - it.c * a.rows;
+      it.there = i < items && (share.column + it.c) % a.q_tiles * 16 + it.r < a.group;
+      return it;
+    };
+    auto finish = [&](const Item& it, float M, float L, f32x4 x) {
+      const u32 col = share.column + it.c, kv_head = col / a.q_tiles;
+      const u32 h = kv_head * a.group + col % a.q_tiles * 16 + it.r;
+      const float v_scale = kF8 && a.d.kv.v_scale ? a.d.kv.v_scale[kv_head] : 1.f;
       x = x * (L == 0.f ? 0.f : v_scale / L);
-      elem* out = (elem*)a.d.out + seq * a.d.out_seq + h * a.d.out_head + qd * 4;
+      elem* out = (elem*)a.d.out + seq * a.d.out_seq + h * a.d.out_head + it.qd * 4;
       typedef elem x4 __attribute__((ext_vector_type(4)));
       *(x4*)out = __builtin_convertvector(x, x4);
-      if (qd == 0 && a.d.lse) a.d.lse[(u64)seq * a.d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
+      if (it.qd == 0 && a.d.lse) a.d.lse[(u64)seq * a.d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
     };
-    for (u32 i = threadIdx.x; i < rows * quads; i += 256) {
-      const u32 r = i / quads, qd = i - r * quads;
+    // where a share's part of a column lies: its second where the row begins within the share
+    auto part_at = [&](u32 share_no, u32 c, bool second) {
+      return ((share_no * a.columns + share.column + c) * 2 + second) * part_size;
+    };
+    for (u32 i = threadIdx.x; i < items; i += 256) {
+      const Item it = item(i);
+      if (!it.there) continue;
       float M = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < (int)kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+      for (u32 w = it.c; w < kWaves; w += together) M = fmaxf(M, s_m[w][it.r]);
       const float ref = M == -INFINITY ? 0.f : M;
       float L = 0.f;
       f32x4 x = 0;
-#pragma unroll
-      for (int w = 0; w < (int)kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
-        L += f * s_l[w][r];
-        x += f * *(const f32x4*)&s_o[w][r][qd * 4];
+      for (u32 w = it.c; w < kWaves; w += together) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w][it.r] - ref);
+        L += f * s_l[w][it.r];
+        x += f * *(const f32x4*)&s_o[w][it.r][it.qd * 4];
       }
       if (whole) {
-        finish(r, qd, ref, L, x);
+        finish(it, ref, L, x);
       } else {
-        put_part(mine, r * D + qd * 4, x);
-        if (qd == 0) put_part(mine, a.rows * D + 2 * r, M, L);
+        const u32 mine = part_at(share.at, it.c, start > share.begin);
+        put_part(parts, mine + it.r * D + it.qd * 4, x);
+        if (it.qd == 0) put_part(parts, mine + a.rows * D + 2 * it.r, M, L);
       }
     }
     if (whole) {
@@ -528,28 +557,24 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
     }
 
     // the row's parts, joined by the workgroup that finishes last; its counter is left at zero
-    const u32 first = (u32)(start / share.per), n_parts = (u32)((next - 1) / share.per) - first + 1;
+    const u32 first = start / share.per, n_parts = (next - 1) / share.per - first + 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has arrived where all workgroups see it
     __syncthreads();
     if (threadIdx.x == 0) {
-      u32* counter = a.counters + seq * a.columns + column;
+      u32* counter = a.counters + (u64)seq * a.columns + share.column;
       const u32 before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       s_last = before == n_parts - 1;
       if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (!s_last) continue;  // (s_last is written again only behind the next row's barriers)
-    // the first part is the second of its share, unless the share begins with the row
-    auto part = [&](u32 k) {
-      const u32 second = k == 0 && start > first * share.per;
-      return part_buffer(a.parts + ((((u64)first + k) * a.columns + column) * 2 + second) * part_size, part_size);
-    };
+    const bool second = start > first * share.per;
     // `crews` of threads take every crews-th part each, eight parts' loads under way
-    const u32 items = rows * quads, crews = items >= 256 ? 1 : 256 / items;
+    const u32 crews = items >= 256 ? 1 : 256 / items;
     for (u32 i0 = 0; i0 < items; i0 += 256) {
-      const u32 i = i0 + (crews > 1 ? threadIdx.x % items : threadIdx.x), crew = crews > 1 ? threadIdx.x / items : 0;
-      const u32 r = i / quads, qd = i - r * quads;
-      const bool works = i < items && crew < crews;
+      const u32 crew = crews > 1 ? threadIdx.x / items : 0, i = i0 + threadIdx.x - crew * items;
+      const Item it = item(i);
+      const bool works = it.there && crew < crews;
       float M = -INFINITY, L = 0.f;
       f32x4 x = 0;
       if (works) {
@@ -558,9 +583,9 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
           v2u32 ml[8];
 #pragma unroll
           for (u32 j = 0; j < 8; ++j) {
-            const u32 k = k0 + j * crews < n_parts ? k0 + j * crews : k0;
-            y[j] = get_part4(part(k), r * D + qd * 4);
-            ml[j] = get_part2(part(k), a.rows * D + 2 * r);
+            const u32 k = k0 + j * crews < n_parts ? k0 + j * crews : k0, from = part_at(first + k, it.c, k == 0 && second);
+            y[j] = get_part4(parts, from + it.r * D + it.qd * 4);
+            ml[j] = get_part2(parts, from + a.rows * D + 2 * it.r);
           }
           float top = M;
 #pragma unroll
@@ -594,20 +619,32 @@ __global__ void __launch_bounds__(256, resident(kDim, kF8)) attend_kernel(Attend
           }
         }
       }
-      if (works && crew == 0) finish(r, qd, M == -INFINITY ? 0.f : M, L, x);
+      if (works && crew == 0) finish(it, M == -INFINITY ? 0.f : M, L, x);
     }
     __syncthreads();  // the next row's sums go where the crews' lay
   }
 }
 
+// As many workgroups as are resident together, fewer where the longest rows that the table allows have not the tiles; a
+// multiple of the columns.
+u32 blocks_of(const Attend& a) {
+  u64 shares = kCus * resident((int)a.d.kv.head_dim) / a.columns;
+  const u64 places = (u64)a.d.n_seqs * ((((u64)a.d.row_pages << a.page_shift) + kTile - 1) / kTile + 1 + kEach);
+  const u64 most = (places + kLeast + kEach - 1) / (kLeast + kEach);
+  if (shares > most) shares = most;
+  return (u32)(shares < 1 ? 1 : shares) * a.columns;
+}
+
 template <typename T, bool kF8, int kDim>
 int launch_attend(const Attend& a, hipStream_t stream) {
-  const u32 blocks = a.shares * a.columns;
+  const u32 blocks = blocks_of(a);
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
   if (a.d.kv.page_tokens < 16)
-    hipLaunchKernelGGL((attend_kernel<T, kF8, kDim, true>), dim3(blocks), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<T, kF8, kDim, true, 0>), dim3(blocks), dim3(256), 0, stream, a);
+  else if (a.q_tiles > 1)
+    hipLaunchKernelGGL((attend_kernel<T, kF8, kDim, false, 0>), dim3(blocks), dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((attend_kernel<T, kF8, kDim, false>), dim3(blocks), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<T, kF8, kDim, false, kNonTemporal>), dim3(blocks), dim3(256), 0, stream, a);
   FDY_HIP_TRY(hipGetLastError());
   return FDY_OK;
 }
@@ -624,7 +661,8 @@ bool sizes_valid(const fdy_attend& d) {
   if (d.kv.head_dim % (d.kv.type == FDY_F8 ? 16 : 8)) return false;
   if (d.n_seqs > 65536u || !d.n_q_heads || d.n_q_heads > 65536u || d.n_q_heads % d.kv.n_heads) return false;
   if ((u64)d.n_seqs * d.n_q_heads > 1u << 22) return false;
-  return (u64)d.row_pages * d.kv.page_tokens < 1ull << 31;
+  const u64 most = (u64)d.row_pages * d.kv.page_tokens;
+  return most < 1ull << 31 && d.n_seqs * most <= 1ull << 36;
 }
 
 // How the call is laid out; the same for the workspace's size and the launch.
@@ -635,12 +673,9 @@ void lay_out(const fdy_attend& d, Attend& a) {
   a.q_tiles = (a.group + 15) / 16;
   a.columns = d.kv.n_heads * a.q_tiles;
   a.rows = a.group < 16 ? a.group : 16;
-  // as many workgroups as are resident together, fewer where the longest rows that the table allows have not the tiles
-  a.shares = kCus * resident((int)d.kv.head_dim, d.kv.type == FDY_F8) / a.columns;
-  if (a.shares < 1) a.shares = 1;
-  const u64 places = (u64)d.n_seqs * ((((u64)d.row_pages << a.page_shift) + kTile - 1) / kTile + 1 + kEach);
-  const u64 most = (places + kLeast + kEach - 1) / (kLeast + kEach);
-  if (a.shares > most) a.shares = most < 1 ? 1 : (u32)most;
+  // heads that lie side by side in a token, and query heads of one cache head, go together
+  const bool beside = d.kv.head_stride < d.kv.token_stride || a.q_tiles > 1;
+  a.together = !beside ? 1 : a.columns % 4 == 0 ? 4 : a.columns % 2 == 0 ? 2 : 1;
 }
 size_t counter_bytes(const Attend& a) { return ((size_t)a.d.n_seqs * a.columns * 4 + 255) / 256 * 256; }
 
@@ -650,7 +685,7 @@ extern "C" size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h) {
   if (!h || !sizes_valid(*h)) return 0;
   Attend a{};
   lay_out(*h, a);
-  const size_t parts = (size_t)a.shares * a.columns * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
+  const size_t parts = (size_t)blocks_of(a) * a.together * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
   return counter_bytes(a) + (parts + 255) / 256 * 256;
 }
 
