@@ -108,7 +108,7 @@ int fdy_rope_frequencies(const fdy_rope* h_rope, double* h_freq);
  * Token strides, head strides: in elements; a head's head_dim elements are contiguous.  kv.head_dim, kv.n_heads give the
  * heads' size and the number of key heads also where no cache is written; kv.type is `type` or FDY_F8.  Any head_dim up to
  * 256 and any even rot_dim up to it are served; rot_dim a multiple of 16, head_dim of 8, and pointers and strides at
- * multiples of 16 bytes (8 elements) take wide accesses. */
+ * multiples of 16 bytes (8 elements) take the widest accesses, half of each the next, anything else single elements. */
 #define FDY_ROPE_HALF 0u
 #define FDY_ROPE_INTERLEAVED 1u
 typedef struct {
@@ -181,8 +181,8 @@ int fdy_paged_attention(const fdy_attend* h_desc, void* d_workspace, size_t work
  * page and row numbers and lengths out of range are skipped and raise FDY_ST_BAD_INDEX; of entries with the same row to
  * be written the first counts, the others are skipped with FDY_ST_BAD_INDEX.
  *   refs, table, lens, rows 4-byte, free_bits, planes, slots 8-byte aligned; planes' addresses, page_bytes, page_stride
- *   multiples of 16; page_tokens a power of two up to 65,536; n_pages, n_rows <= 2^28, row_pages <= 2^25,
- *   row_pages * page_tokens < 2^31, n_planes <= 2^20 */
+ *   multiples of 16, page_bytes < 2^30; page_tokens a power of two up to 65,536; n_pages, n_rows <= 2^28, row_pages <= 2^25,
+ *   row_pages * page_tokens < 2^31, n_planes <= 32,768 */
 typedef struct {
   uint32_t* refs;      /* [n_pages]              */
   uint64_t* free_bits; /* [ceil(n_pages / 64)]   */

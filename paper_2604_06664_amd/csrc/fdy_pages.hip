@@ -22,7 +22,8 @@ struct PagesArg {
   int32_t* map;
   u32* n_live;
   u32* ws;  // words of the workspace, laid out by each call
-  u32 n, n_slots, shift, slices;
+  u32 n, n_slots, shift, slices, pieces;  // pieces: of a page in a plane
+  u32 fill;
 };
 typedef Arg<PagesArg> Pages;
 
@@ -58,18 +59,21 @@ __device__ __forceinline__ bool named_before(const int32_t* list, u32 i) {
   return __syncthreads_or(found);
 }
 
-// The contents of a page of one plane, by the threads of a workgroup.
-__device__ __forceinline__ void copy_page(const Pages& a, u32 plane, u32 src, u32 dst) {
-  const u64 base = a.d.planes[plane];
-  const v4u32* s = (const v4u32*)(base + src * a.d.page_stride);
-  v4u32* d = (v4u32*)(base + dst * a.d.page_stride);
-  const u64 n = a.d.page_bytes / 16;
-  u64 i = threadIdx.x;
-  for (; i + 3 * 256 < n; i += 4 * 256) {
-    const v4u32 x0 = s[i], x1 = s[i + 256], x2 = s[i + 512], x3 = s[i + 768];
-    d[i] = x0, d[i + 256] = x1, d[i + 512] = x2, d[i + 768] = x3;
-  }
-  for (; i < n; i += 256) d[i] = s[i];
+// One piece of a page's contents in one plane, by the threads of a workgroup: two 16-byte loads each under way.  The bound is
+// memory.  Stores are marked as not to be kept, which what is copied (read a step later at the earliest) does not need: 25,920
+// pages for an extend 180 us without, 168 with; loads are marked where no page is a source twice (184 us where three beams
+// copy one page).
+constexpr u32 kPiece = 256 * 2 * 16;
+template <bool kOnce>
+__device__ __forceinline__ void copy_piece(const Pages& a, u32 plane, u32 src, u32 dst, u32 piece) {
+  const u64 base = a.d.planes[plane], at = (u64)piece * kPiece, left = a.d.page_bytes - at;
+  const u32 n = (u32)(left < kPiece ? left : kPiece), i = threadIdx.x * 16;
+  const auto s = buffer((const void*)(base + src * a.d.page_stride + at), n), d = buffer((const void*)(base + dst * a.d.page_stride + at), n);
+  v4u32 x[2];
+#pragma unroll
+  for (u32 j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_raw_buffer_load_b128(s, i + j * 4096, 0, kOnce ? kNonTemporal : 0);
+#pragma unroll
+  for (u32 j = 0; j < 2; ++j) __builtin_amdgcn_raw_buffer_store_b128(x[j], d, i + j * 4096, 0, kNonTemporal);
 }
 
 // ---- reset ------------------------------------------------------------------------------------------
@@ -105,6 +109,52 @@ __device__ __forceinline__ ExtendWords extend_layout(const Pages& a) {
   w.rank = w.need + a.n;
   w.copy = w.rank + a.n;
   return w;
+}
+
+// What an entry of the list wants, and its pages' first number among those found.
+struct Entry {
+  u32 row, count, length, last, need, rank;
+  bool copies, fits;
+};
+
+// Gives entry i its pages, if they were found, and writes its slot and position where it has one token.
+template <typename Taken>
+__device__ __forceinline__ void serve(const Pages& a, const ExtendWords& w, u32 i, const Entry& e, u32 found, Taken taken,
+                                      u32* s_served, u32& wrong) {
+  bool served = e.fits;
+  if (served && e.need && (u64)e.rank + e.need > found) wrong |= FDY_ST_CAPACITY, served = false;
+  u32 copy = kNoPage;
+  int32_t* table = a.d.table + (u64)(served ? e.row : 0) * a.d.row_pages;
+  u32 at_end = kNoPage;  // page of the first new token
+  if (served) {
+    const u32 before = pages_of(a, e.length), end = e.rank + e.need;
+    u32 at = e.rank;
+    if (e.copies) {
+      copy = taken(at);
+      table[before - 1] = (int32_t)copy;
+      atomicSub(a.d.refs + e.last, 1u);
+      ++at;
+    }
+    for (u32 j = before; at < end; ++at, ++j) table[j] = (int32_t)taken(at);
+    for (at = e.rank; at < end; ++at) a.d.refs[taken(at)] = 1;
+    a.d.lens[e.row] = (int32_t)(e.length + e.count);
+    if (e.need) {
+      atomicMax(s_served, end);
+      at_end = taken(e.rank);
+    }
+  }
+  if (a.d.n_planes || a.to) {  // for the launch that follows
+    w.copy[i] = copy;
+    w.last[i] = e.last;
+    w.length[i] = e.length | (served ? 0 : kUnserved);
+  }
+  if (!a.to && i < a.n_slots) {
+    if (a.slots) {
+      if (served && at_end == kNoPage) at_end = (u32)table[e.length >> a.shift];
+      a.slots[i] = served ? (int64_t)at_end * a.d.page_tokens + e.length % a.d.page_tokens : -1;
+    }
+    if (a.positions) a.positions[i] = (int32_t)e.length;
+  }
 }
 
 // One workgroup keeps the books.
@@ -193,39 +243,115 @@ __global__ void __launch_bounds__(kBooksThreads) extend_books_kernel(Pages a) {
   __syncthreads();
   // the rows that get theirs
   for (u32 i = tid; i < a.n; i += kBooksThreads) {
-    const u32 need = w.need[i] & ~kCopies, rank = w.rank[i], row = row_of(i), count = a.to ? (u32)a.to[i] : 1u;
-    const bool copies = w.need[i] & kCopies;
-    u32 length = w.length[i];
-    bool served = !(length & kUnserved);
-    if (served && need && (u64)rank + need > found) wrong |= FDY_ST_CAPACITY, served = false;
-    length &= ~kUnserved;
-    u32 copy = kNoPage;
-    if (served) {
-      int32_t* table = a.d.table + (u64)row * a.d.row_pages;
-      const u32 before = pages_of(a, length);
-      u32 at = rank, end = rank + need;
-      if (copies) {
-        copy = w.taken[at];
-        table[before - 1] = (int32_t)copy;
-        atomicSub(a.d.refs + w.last[i], 1u);
-        ++at;
-      }
-      for (u32 j = before; at < end; ++at, ++j) table[j] = (int32_t)w.taken[at];
-      for (at = rank; at < end; ++at) a.d.refs[w.taken[at]] = 1;
-      a.d.lens[row] = (int32_t)(length + count);
-      if (need) atomicMax(&s_served, rank + need);
-    }
-    w.copy[i] = copy;
-    w.length[i] = length | (served ? 0 : kUnserved);
-    if (!a.to && i < a.n_slots) {  // one token each: its slot and position
-      if (a.slots)
-        a.slots[i] = served ? (int64_t)a.d.table[(u64)row * a.d.row_pages + (length >> a.shift)] * pt + length % pt : -1;
-      if (a.positions) a.positions[i] = (int32_t)length;
-    }
+    Entry e;
+    e.row = row_of(i), e.count = a.to ? (u32)a.to[i] : 1u, e.length = w.length[i] & ~kUnserved, e.last = w.last[i];
+    e.need = w.need[i] & ~kCopies, e.rank = w.rank[i], e.copies = w.need[i] & kCopies, e.fits = !(w.length[i] & kUnserved);
+    serve(a, w, i, e, (u32)found, [&](u32 r) { return w.taken[r]; }, &s_served, wrong);
   }
   __syncthreads();
   for (u32 r = tid; r < s_served; r += kBooksThreads) {
     const u32 page = w.taken[r];
+    atomicAnd((u32*)a.d.free_bits + (page >> 5), ~(1u << (page & 31)));
+  }
+  if (wrong) raise_status(a.status, wrong);
+}
+
+// The same for up to 1,024 entries, one a thread, which keeps what it knows in registers; who names a row first and who asks
+// for a page are counted in LDS, by hashing (512 rows: 20 us through the workspace, 14 so).
+constexpr u32 kHash = 2048, kTakenHere = 4096;
+struct Counts {
+  u32 key[kHash], sum[kHash], top[kHash];
+};
+__device__ __forceinline__ void clear(Counts& c) {
+  for (u32 i = threadIdx.x; i < kHash; i += kBooksThreads) c.key[i] = ~0u, c.sum[i] = 0, c.top[i] = 0;
+}
+__device__ __forceinline__ u32 place_of(Counts& c, u32 key) {  // at most half full: ends
+  u32 at = key * 0x9e3779b1u >> 21;
+  for (;; at = (at + 1) % kHash) {
+    const u32 there = atomicCAS(&c.key[at], ~0u, key);
+    if (there == ~0u || there == key) return at;
+  }
+}
+
+__global__ void __launch_bounds__(kBooksThreads) extend_few_kernel(Pages a) {
+  __shared__ u64 s_scan[17];
+  __shared__ Counts s_rows, s_pages;
+  __shared__ u32 s_taken[kTakenHere];
+  __shared__ u32 s_served;
+  const ExtendWords w = extend_layout(a);
+  const u32 i = threadIdx.x, pt = a.d.page_tokens, words = (a.d.n_pages + 63) / 64;
+  u32 wrong = 0;
+  u64 bits = i < words ? a.d.free_bits[i] : 0;  // the first pages' are asked for ahead of all else
+  const bool there = i < a.n;
+  Entry e{};
+  e.last = kNoPage;
+  e.row = there ? (a.from ? (u32)a.from[i] : i) : ~0u;
+  int count = there ? (a.to ? a.to[i] : 1) : 0;
+  if (count < 0) wrong |= FDY_ST_BAD_INDEX, count = 0;
+  e.count = (u32)count;
+  bool good = there && e.row < a.d.n_rows;
+  if (good) {
+    bool bad = false;
+    e.length = length_of(a, e.row, bad);
+    if (e.length % pt) {
+      e.last = (u32)a.d.table[(u64)e.row * a.d.row_pages + (e.length >> a.shift)];
+      bad |= e.last >= a.d.n_pages;
+    }
+    if (bad) good = false;
+  }
+  u32 holders = good && e.last != kNoPage ? a.d.refs[e.last] : 0;
+  clear(s_pages);
+  if (a.from) clear(s_rows);
+  if (i == 0) s_served = 0;
+  u64 sum, begin = i;
+  if (a.to)
+    begin = block_excl_scan(e.count, s_scan, sum);
+  else
+    __syncthreads();
+  u32 row_at = 0;
+  if (a.from) {
+    if (there && e.row < a.d.n_rows) row_at = place_of(s_rows, e.row), atomicMax(&s_rows.top[row_at], a.n - i);
+    __syncthreads();
+    good = good && s_rows.top[row_at] == a.n - i;
+  }
+  if (!good) e.length = 0;
+  if (there && !good) wrong |= FDY_ST_BAD_INDEX;
+  e.fits = good && count > 0;
+  if (e.fits && ((u64)e.length + e.count > a.d.row_pages << a.shift || begin + e.count > a.n_slots)) wrong |= FDY_ST_CAPACITY, e.fits = false;
+  const bool shared = e.fits && e.last != kNoPage && holders > 1;
+  if (!shared) e.last = kNoPage;
+  u32 page_at = 0;
+  if (shared) page_at = place_of(s_pages, e.last), atomicAdd(&s_pages.sum[page_at], 1u), atomicMax(&s_pages.top[page_at], i + 1);
+  __syncthreads();
+  e.copies = shared && !(s_pages.sum[page_at] == holders && s_pages.top[page_at] == i + 1);
+  if (e.fits) e.need = pages_of(a, e.length + e.count) - pages_of(a, e.length) + e.copies;
+  u64 total;
+  const u64 rank = block_excl_scan(e.need, s_scan, total);
+  e.rank = rank < a.d.n_pages ? (u32)rank : a.d.n_pages;
+  u64 found = 0;
+  for (u32 w0 = 0; w0 < words && found < total; w0 += kBooksThreads) {
+    if (w0) bits = w0 + i < words ? a.d.free_bits[w0 + i] : 0;
+    if (w0 + i == words - 1 && a.d.n_pages % 64) bits &= (1ull << a.d.n_pages % 64) - 1;
+    u64 r = found + block_excl_scan((u64)__popcll(bits), s_scan, sum);
+    found += sum;
+    for (; bits && r < total; bits &= bits - 1, ++r) {
+      const u32 page = (w0 + i) * 64 + (u32)__builtin_ctzll(bits);
+      if (r < kTakenHere)
+        s_taken[r] = page;
+      else
+        w.taken[r] = page;
+    }
+  }
+  if (found > total) found = total;
+  __syncthreads();
+  const auto taken = [&](u32 r) { return r < kTakenHere ? s_taken[r] : w.taken[r]; };
+  if (there) {
+    if (a.to) w.begin[i] = begin < a.n_slots ? (u32)begin : a.n_slots;
+    serve(a, w, i, e, (u32)found, taken, &s_served, wrong);
+  }
+  __syncthreads();
+  for (u32 r = i; r < s_served; r += kBooksThreads) {
+    const u32 page = taken(r);
     atomicAnd((u32*)a.d.free_bits + (page >> 5), ~(1u << (page & 31)));
   }
   if (wrong) raise_status(a.status, wrong);
@@ -237,7 +363,7 @@ __global__ void __launch_bounds__(256) extend_copy_kernel(Pages a) {
   const u32 i = blockIdx.x, copy = w.copy[i];
   if (copy != kNoPage) {
     const u32 src = w.last[i];
-    for (u32 p = blockIdx.y; p < a.d.n_planes; p += gridDim.y) copy_page(a, p, src, copy);
+    for (u32 t = blockIdx.y; t < a.d.n_planes * a.pieces; t += gridDim.y) copy_piece<false>(a, t / a.pieces, src, copy, t % a.pieces);
   }
   if (!a.to || blockIdx.y) return;
   const u32 row = a.from ? (u32)a.from[i] : i;
@@ -259,25 +385,35 @@ __host__ __device__ inline u64 fork_words(const fdy_pages& d, u32 n) { return (u
 constexpr u32 kForkPages = 1024;  // pages of a row a workgroup takes
 
 __global__ void __launch_bounds__(256) fork_note_kernel(Pages a) {
-  const u32 i = blockIdx.x, s = (u32)a.from[i], d = (u32)a.to[i];
-  const bool good = s < a.d.n_rows && d < a.d.n_rows && !named_before(a.to, i);
+  constexpr u32 kMine = kForkPages / 256;
+  const u32 i = blockIdx.x, s = (u32)a.from[i], d = (u32)a.to[i], j0 = blockIdx.y * kForkPages + threadIdx.x;
+  const bool in = s < a.d.n_rows && d < a.d.n_rows;
   u32* lens = a.ws + (u64)a.n * a.d.row_pages + 2 * i;
-  if (!good) {
+  // what the row holds and held is asked for before the list is searched
+  bool bad = false;
+  const u32 now = in ? length_of(a, s, bad) : 0, old = in ? length_of(a, d, bad) : 0, n = pages_of(a, now), n_old = pages_of(a, old);
+  const int32_t *src = a.d.table + (u64)s * a.d.row_pages, *dst = a.d.table + (u64)d * a.d.row_pages;
+  u32 p[kMine], q[kMine];
+#pragma unroll
+  for (u32 k = 0; k < kMine; ++k) {
+    const u32 j = j0 + k * 256;
+    p[k] = j < n ? (u32)src[j] : kNoPage;
+    q[k] = j < n && j < n_old ? (u32)dst[j] : kNoPage;
+  }
+  if (!in || named_before(a.to, i)) {
     if (threadIdx.x == 0 && blockIdx.y == 0) lens[0] = kUnserved, raise_status(a.status, FDY_ST_BAD_INDEX);
     return;
   }
-  bool bad = false;
-  const u32 now = length_of(a, s, bad), old = length_of(a, d, bad), n = pages_of(a, now), n_old = pages_of(a, old);
   if (threadIdx.x == 0 && blockIdx.y == 0) lens[0] = now, lens[1] = old;
-  const int32_t *src = a.d.table + (u64)s * a.d.row_pages, *dst = a.d.table + (u64)d * a.d.row_pages;
   u32* noted = a.ws + (u64)i * a.d.row_pages;
-  const u32 end = n < (blockIdx.y + 1) * kForkPages ? n : (blockIdx.y + 1) * kForkPages;
-  for (u32 j = blockIdx.y * kForkPages + threadIdx.x; j < end; j += 256) {
-    const u32 p = (u32)src[j];
-    noted[j] = p;
-    if (j < n_old && (u32)dst[j] == p) continue;
-    if (p < a.d.n_pages)
-      atomicAdd(a.d.refs + p, 1u);
+#pragma unroll
+  for (u32 k = 0; k < kMine; ++k) {
+    const u32 j = j0 + k * 256;
+    if (j >= n) break;
+    noted[j] = p[k];
+    if (p[k] == q[k] && j < n_old) continue;
+    if (p[k] < a.d.n_pages)
+      atomicAdd(a.d.refs + p[k], 1u);
     else
       bad = true;
   }
@@ -329,7 +465,7 @@ __global__ void __launch_bounds__(256) copy_kernel(Pages a) {
     if (threadIdx.x == 0 && blockIdx.y == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
     return;
   }
-  for (u32 p = blockIdx.y; p < a.d.n_planes; p += gridDim.y) copy_page(a, p, s, d);
+  for (u32 t = blockIdx.y; t < a.d.n_planes * a.pieces; t += gridDim.y) copy_piece<false>(a, t / a.pieces, s, d, t % a.pieces);
 }
 
 // ---- compact ----------------------------------------------------------------------------------------
@@ -390,15 +526,17 @@ __global__ void __launch_bounds__(kBooksThreads) compact_plan_kernel(Pages a) {
   }
 }
 
-// The first `slices` workgroups keep the books, the others copy pages.
+// The first `slices` workgroups keep the books, the others copy pieces of pages, plane after plane.
 __global__ void __launch_bounds__(256) compact_move_kernel(Pages a) {
   const CompactWords w = compact_layout(a);
   const u32 moves = w.counts[0], n_live = w.counts[1];
   if (blockIdx.x >= a.slices) {
-    const u64 tasks = (u64)moves * a.d.n_planes;
+    const u64 of_plane = (u64)moves * a.pieces, tasks = of_plane * a.d.n_planes;
     for (u64 t = blockIdx.x - a.slices; t < tasks; t += gridDim.x - a.slices) {
-      const u32 k = (u32)(t / a.d.n_planes), plane = (u32)(t - (u64)k * a.d.n_planes);
-      copy_page(a, plane, w.movers[k], w.holes[k]);
+      const u32 plane = tasks >> 32 ? (u32)(t / of_plane) : (u32)t / (u32)of_plane;
+      const u64 rest = t - plane * of_plane;
+      const u32 k = rest >> 32 ? (u32)(rest / a.pieces) : (u32)rest / a.pieces;
+      copy_piece<true>(a, plane, w.movers[k], w.holes[k], (u32)(rest - (u64)k * a.pieces));
     }
     return;
   }
@@ -435,8 +573,8 @@ __global__ void __launch_bounds__(256) compact_move_kernel(Pages a) {
 bool pages_valid(const fdy_pages& d) {
   if (d.reserved || !d.n_pages || d.n_pages > 1u << 28 || d.n_rows > 1u << 28 || d.row_pages > 1u << 25) return false;
   if (!power_of_two(d.page_tokens) || d.page_tokens > 65536u || (u64)d.row_pages * d.page_tokens >= 1ull << 31) return false;
-  if (d.n_planes && (d.page_bytes % 16 || d.page_stride % 16 || d.page_bytes >> 40 || d.page_stride >> 40)) return false;
-  return d.n_planes <= 1u << 20;
+  if (d.n_planes && (d.page_bytes % 16 || d.page_stride % 16 || d.page_bytes >> 30 || d.page_stride >> 40)) return false;
+  return d.n_planes <= 32768u;
 }
 
 // `pages`: the call takes or gives pages; `rows`: it reads rows; `planes`: it moves contents
@@ -456,6 +594,7 @@ Pages args(const fdy_pages* h, u32 n, void* ws, u32* status) {
   a.ws = (u32*)ws;
   a.status = status;
   a.shift = log2_of(h->page_tokens);
+  a.pieces = (u32)((h->page_bytes + kPiece - 1) / kPiece);
   return a;
 }
 
@@ -500,9 +639,10 @@ extern "C" int fdy_pages_extend(const fdy_pages* h, const int32_t* d_rows, const
   if (workspace_bad(h, n, ws, ws_bytes)) return FDY_ERR_WORKSPACE;
   Pages a = args(h, n, ws, d_status);
   a.from = d_rows, a.to = d_counts, a.slots = d_slots, a.positions = d_positions, a.n_slots = n_slots;
-  rc = go(extend_books_kernel, dim3(1), kBooksThreads, stream, a);
+  rc = n <= kBooksThreads ? go(extend_few_kernel, dim3(1), kBooksThreads, stream, a)
+                          : go(extend_books_kernel, dim3(1), kBooksThreads, stream, a);
   if (rc != FDY_OK || (!h->n_planes && !d_counts)) return rc;
-  return go(extend_copy_kernel, dim3(n, at_most(h->n_planes ? h->n_planes : 1, 256)), 256, stream, a);
+  return go(extend_copy_kernel, dim3(n, at_most((u64)h->n_planes * a.pieces + (h->n_planes * a.pieces == 0), 1024)), 256, stream, a);
 }
 
 extern "C" int fdy_pages_fork(const fdy_pages* h, const int32_t* d_src, const int32_t* d_dst, uint32_t n, void* ws,
@@ -540,7 +680,7 @@ extern "C" int fdy_pages_copy(const fdy_pages* h, const int32_t* d_src, const in
   if (!d_src || !d_dst) return FDY_ERR_INVALID_ARG;
   Pages a = args(h, n, nullptr, d_status);
   a.from = d_src, a.to = d_dst;
-  return go(copy_kernel, dim3(n, at_most(h->n_planes, 256)), 256, stream, a);
+  return go(copy_kernel, dim3(n, at_most((u64)h->n_planes * a.pieces + (a.pieces == 0), 1024)), 256, stream, a);
 }
 
 extern "C" int fdy_pages_compact(const fdy_pages* h, int32_t* d_map, uint32_t* d_n_live, void* ws, size_t ws_bytes,
@@ -553,9 +693,9 @@ extern "C" int fdy_pages_compact(const fdy_pages* h, int32_t* d_map, uint32_t* d
   a.map = d_map, a.n_live = d_n_live;
   rc = go(compact_plan_kernel, dim3(1), kBooksThreads, stream, a);
   if (rc != FDY_OK) return rc;
-  // books: a workgroup a row or 1,024 pages; contents: as many as fill the chip, or fewer where there cannot be as many moves
-  const u32 books = h->n_rows > (h->n_pages + 1023) / 1024 ? h->n_rows : (h->n_pages + 1023) / 1024;
-  a.slices = at_most(books, 1024);
-  const u32 movers = h->n_planes ? at_most((u64)(h->n_pages / 2 + 1) * h->n_planes, 256 * 8) : 0;
-  return go(compact_move_kernel, dim3(a.slices + movers), 256, stream, a);
+  // books: a workgroup a row or 1,024 pages.  Contents: up to 65,536 workgroups, the next piece to the next (158,400 pieces of
+  // 16 KiB: 605 us, and 645 with 4,096 workgroups, 690 with 2,048 that go round); more would cost where little is to be moved
+  a.slices = at_most(h->n_rows > h->n_pages / 1024 ? h->n_rows : h->n_pages / 1024 + 1, 1024);
+  const u32 copiers = at_most((u64)(h->n_pages / 2 + 1) * (h->n_planes ? a.pieces : 0) * h->n_planes, 65536);
+  return go(compact_move_kernel, dim3(a.slices + copiers), 256, stream, a);
 }

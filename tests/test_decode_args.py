@@ -138,7 +138,7 @@ def page_calls(d, names, ws=A, size=1 << 50):
 @pytest.mark.parametrize("kw", [dict(reserved=1), dict(n_pages=0), dict(n_pages=(1 << 28) + 1), dict(n_rows=(1 << 28) + 1),
                                 dict(page_tokens=0), dict(page_tokens=48), dict(page_tokens=1 << 17), dict(row_pages=(1 << 25) + 1),
                                 dict(row_pages=1 << 24, page_tokens=128), dict(page_bytes=24), dict(page_stride=8),
-                                dict(page_bytes=1 << 41), dict(n_planes=(1 << 20) + 1)])
+                                dict(page_bytes=1 << 30), dict(n_planes=32769)])
 def test_pages_refuse_sizes(kw):
     d = pages(**kw)
     assert fdd.fdy_pages_workspace_bytes(d, 3) == 0
