@@ -38,35 +38,40 @@ struct AppendArg {
 };
 typedef Arg<AppendArg> Append;
 
-template <typename T>
-__device__ __forceinline__ f32x8 widen(typename T::x8 x) {
-  return __builtin_convertvector(x, f32x8);
-}
+template <typename T, int kN>
+struct Chunk {
+  typedef typename T::elem raw __attribute__((ext_vector_type(kN)));
+  typedef float wide __attribute__((ext_vector_type(kN)));
+};
 
-// 8 elements to a cache: rounded once, to the cache's type.
-template <typename T, bool kF8>
-__device__ __forceinline__ void put8(void* base, u64 at, f32x8 x, float inv) {
+// A chunk of elements to a cache: rounded once, to the cache's type.
+template <typename T, int kN, bool kF8>
+__device__ __forceinline__ void put(void* base, u64 at, typename Chunk<T, kN>::wide x, float inv) {
   if (kF8) {
-    const v2u32 w = {to_f8x4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
-                     to_f8x4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv)};
-    *(v2u32*)((uint8_t*)base + at) = w;
+    typedef u32 words __attribute__((ext_vector_type(kN / 4)));
+    words w;
+#pragma unroll
+    for (int i = 0; i < kN / 4; ++i) w[i] = to_f8x4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
+    *(words*)((uint8_t*)base + at) = w;
   } else {
-    *(typename T::x8*)((typename T::elem*)base + at) = __builtin_convertvector(x, typename T::x8);
+    typedef typename Chunk<T, kN>::raw raw;
+    *(raw*)((typename T::elem*)base + at) = __builtin_convertvector(x, raw);
   }
 }
 
-__device__ __forceinline__ void turn(f32x8& a, f32x8& b, f32x8 cs, f32x8 sn, bool half) {
-  const f32x8 x = a, y = b;
+template <typename V, int kN>
+__device__ __forceinline__ void turn(V& a, V& b, V cs, V sn, bool half) {
+  const V x = a, y = b;
   if (half) {
     a = x * cs - y * sn;
     b = y * cs + x * sn;
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kN / 2; ++i) {
       a[2 * i] = x[2 * i] * cs[i] - x[2 * i + 1] * sn[i];
       a[2 * i + 1] = x[2 * i + 1] * cs[i] + x[2 * i] * sn[i];
-      b[2 * i] = y[2 * i] * cs[4 + i] - y[2 * i + 1] * sn[4 + i];
-      b[2 * i + 1] = y[2 * i + 1] * cs[4 + i] + y[2 * i] * sn[4 + i];
+      b[2 * i] = y[2 * i] * cs[kN / 2 + i] - y[2 * i + 1] * sn[kN / 2 + i];
+      b[2 * i + 1] = y[2 * i + 1] * cs[kN / 2 + i] + y[2 * i] * sn[kN / 2 + i];
     }
   }
 }
@@ -121,11 +126,13 @@ __device__ __forceinline__ bool slot_of(const Append& a, u32 t, u64& page, u32& 
   return in;
 }
 
-// A wave takes a token; a lane takes 16 elements of a head at a time (two 16-byte loads: the two halves of eight pairs) and
-// keeps their eight cosines and sines in registers over all heads that it visits.
-template <typename T, bool kF8>
+// A wave takes a token; a lane takes 2 kN elements of a head at a time (two loads of kN: the two halves of kN pairs) and keeps
+// their kN cosines and sines in registers over all heads that it visits.  kN is 8, or 4 where heads, halves or addresses are
+// multiples of 8 bytes only (4,096 tokens of 32 + 8 heads of 80, of which 40 turned: 161 us one element a thread).
+template <typename T, int kN, bool kF8>
 __global__ void __launch_bounds__(256) append_kernel(Append a) {
-  typedef typename T::x8 x8;
+  typedef typename Chunk<T, kN>::raw raw;
+  typedef typename Chunk<T, kN>::wide wide;
   typedef typename T::elem elem;
   const u32 t = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= a.d.n_tokens) return;
@@ -140,20 +147,20 @@ __global__ void __launch_bounds__(256) append_kernel(Append a) {
   u64 page = 0;
   u32 place = 0;
   const bool stored = slot_of(a, t, page, place, lane == 0 ? a.status : nullptr);
-  if (u * 16 >= D) return;
-  const bool turns = u < rot / 16;
-  f32x8 cs = 0, sn = 0;
+  if (u * 2 * kN >= D) return;
+  const bool turns = u < rot / (2 * kN);
+  wide cs = 0, sn = 0;
   if (turns) {
-    const float* row = a.d.table + (u64)p * rot + u * 8;
-    cs = *(const f32x8*)row;
-    sn = *(const f32x8*)(row + rot / 2);
+    const float* row = a.d.table + (u64)p * rot + u * kN;
+    cs = *(const wide*)row;
+    sn = *(const wide*)(row + rot / 2);
   }
   // offsets of the two chunks in a turned head, and in one that is copied
-  const u32 ta = turns && half ? u * 8 : u * 16, tb = turns && half ? rot / 2 + u * 8 : u * 16 + 8, va = u * 16, vb = va + 8;
+  const u32 va = u * 2 * kN, vb = va + kN, ta = turns && half ? u * kN : va, tb = turns && half ? rot / 2 + u * kN : vb;
   const u32 n = a.n_heads, stride = step * a.slices;
-  constexpr int kDeep = 4;
+  constexpr int kDeep = 2;  // heads under way at once (four: into 8 bits 182 us for 177)
   for (u32 h0 = hs + blockIdx.y * step; h0 < n; h0 += stride * kDeep) {
-    x8 xa[kDeep], xb[kDeep];
+    raw xa[kDeep], xb[kDeep];
     Route r[kDeep];
 #pragma unroll
     for (int i = 0; i < kDeep; ++i) {
@@ -161,24 +168,24 @@ __global__ void __launch_bounds__(256) append_kernel(Append a) {
       if (h >= n) continue;
       r[i] = route_of<kF8>(a, t, h, stored, page, place);
       const elem* src = (const elem*)r[i].src + r[i].from;
-      xa[i] = *(const x8*)(src + (r[i].turned ? ta : va));
+      xa[i] = *(const raw*)(src + (r[i].turned ? ta : va));
       const u32 b = r[i].turned ? tb : vb;
-      if (b < D) xb[i] = *(const x8*)(src + b);
+      if (b < D) xb[i] = *(const raw*)(src + b);
     }
 #pragma unroll
     for (int i = 0; i < kDeep; ++i) {
       const u32 h = h0 + i * stride;
       if (h >= n) continue;
-      f32x8 fa = widen<T>(xa[i]), fb = widen<T>(xb[i]);
-      if (r[i].turned && turns) turn(fa, fb, cs, sn, half);
+      wide fa = __builtin_convertvector(xa[i], wide), fb = __builtin_convertvector(xb[i], wide);
+      if (r[i].turned && turns) turn<wide, kN>(fa, fb, cs, sn, half);
       const u32 at = r[i].turned ? ta : va, bt = r[i].turned ? tb : vb;
       if (r[i].out) {
-        put8<T, false>(r[i].out, r[i].to + at, fa, 1.f);
-        if (bt < D) put8<T, false>(r[i].out, r[i].to + bt, fb, 1.f);
+        put<T, kN, false>(r[i].out, r[i].to + at, fa, 1.f);
+        if (bt < D) put<T, kN, false>(r[i].out, r[i].to + bt, fb, 1.f);
       }
       if (r[i].cache) {
-        put8<T, kF8>(r[i].cache, r[i].in_cache + at, fa, r[i].inv);
-        if (bt < D) put8<T, kF8>(r[i].cache, r[i].in_cache + bt, fb, r[i].inv);
+        put<T, kN, kF8>(r[i].cache, r[i].in_cache + at, fa, r[i].inv);
+        if (bt < D) put<T, kN, kF8>(r[i].cache, r[i].in_cache + bt, fb, r[i].inv);
       }
     }
   }
@@ -230,22 +237,26 @@ __global__ void __launch_bounds__(256) append_any_kernel(Append a) {
   }
 }
 
+// `wide`: elements of an access, 8, 4 or 1
 template <typename T, bool kF8>
-int launch_append(const Append& a, bool wide, u32 n_cu, hipStream_t stream) {
+int launch_append(const Append& a, u32 wide, u32 n_cu, hipStream_t stream) {
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
-  const u32 T_ = a.d.n_tokens;
-  if (wide) {
+  const u32 n = a.d.n_tokens;
+  if (wide > 1) {
     Append b = a;
     b.unit_shift = 0;
-    while ((16u << b.unit_shift) < a.d.kv.head_dim) ++b.unit_shift;
-    // heads a wave visits one after another are spread over more waves until the chip has eight a SIMD
-    const u32 step = 64u >> b.unit_shift, rounds = (a.n_heads + step - 1) / step;
-    u32 slices = (n_cu * 32 + T_ - 1) / T_;
+    while ((2 * wide << b.unit_shift) < a.d.kv.head_dim) ++b.unit_shift;
+    // heads that a wave visits one after another are spread over more waves where these would be less than four a SIMD
+    const u32 step = 64u >> b.unit_shift, rounds = (a.n_heads + step - 1) / step, slices = n_cu * 16 / n;
     b.slices = slices < 1 ? 1 : slices > rounds ? rounds : slices;
-    hipLaunchKernelGGL((append_kernel<T, kF8>), dim3((T_ + 3) / 4, b.slices), dim3(256), 0, stream, b);
+    const dim3 grid((n + 3) / 4, b.slices);
+    if (wide == 8)
+      hipLaunchKernelGGL((append_kernel<T, 8, kF8>), grid, dim3(256), 0, stream, b);
+    else
+      hipLaunchKernelGGL((append_kernel<T, 4, kF8>), grid, dim3(256), 0, stream, b);
   } else {
     const u32 y = a.n_heads < 1024 ? a.n_heads : 1024;
-    hipLaunchKernelGGL((append_any_kernel<T, kF8>), dim3(T_, y), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((append_any_kernel<T, kF8>), dim3(n, y), dim3(256), 0, stream, a);
   }
   FDY_HIP_TRY(hipGetLastError());
   return FDY_OK;
@@ -334,16 +345,17 @@ extern "C" int fdy_rope_append(const fdy_append* h, uint32_t* d_status, void* st
   a.unit_shift = 0;
   a.slices = 1;
   a.n_heads = (d.q ? d.n_q_heads : 0) + d.kv.n_heads * (d.slots ? 2 : 1);
-  bool wide = d.rot_dim % 16 == 0 && d.kv.head_dim % 8 == 0;
-  for (const void* p : elems) wide = wide && aligned(p, 16);
   u64 strides = d.k_token | d.k_head;
   if (d.q) strides |= d.q_token | d.q_head | d.q_out_token | d.q_out_head;
   if (d.k_out) strides |= d.k_out_token | d.k_out_head;
-  if (d.slots) {
-    strides |= d.v_token | d.v_head | d.kv.page_stride | d.kv.token_stride | d.kv.head_stride;
-    wide = wide && aligned(d.kv.k, 8 * cache_bytes) && aligned(d.kv.v, 8 * cache_bytes);
+  if (d.slots) strides |= d.v_token | d.v_head | d.kv.page_stride | d.kv.token_stride | d.kv.head_stride;
+  u32 wide = 8;  // elements of an access that sizes, strides and addresses allow
+  for (; wide > 1; wide = wide == 8 ? 4 : 1) {
+    bool fits = d.rot_dim % (2 * wide) == 0 && d.kv.head_dim % wide == 0 && strides % wide == 0;
+    for (const void* p : elems) fits = fits && aligned(p, 2 * wide);
+    if (d.slots) fits = fits && aligned(d.kv.k, wide * cache_bytes) && aligned(d.kv.v, wide * cache_bytes);
+    if (fits) break;
   }
-  wide = wide && strides % 8 == 0;
   int dev, n_cu;
   const int rc = current_device(&dev, &n_cu);
   if (rc != FDY_OK) return rc;
