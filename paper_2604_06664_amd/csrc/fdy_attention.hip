@@ -21,8 +21,7 @@ using namespace fdy;
 namespace {
 
 constexpr u32 kWaves = 4, kTile = 32, kCus = 256;
-constexpr u32 kLeast = 4;  // tiles of a share, at least: one for each wave
-constexpr u32 kEach = 3;   // what a row costs beside its tiles (queries, join, output), in tiles
+constexpr u32 kEach = 3;  // what a row costs beside its tiles (queries, join, output), in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArg {
@@ -30,8 +29,10 @@ struct AttendArg {
   u32* status;
   u32* counters;  // [n_seqs][columns], zero between calls
   float* parts;   // [shares][columns][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
-  // columns: cache heads x q_tiles; rows: query heads of a tile; together: columns that a workgroup may take at once
-  u32 page_shift, group, q_tiles, columns, rows, together;
+  // columns: cache heads x q_tiles; rows: query heads of a tile; together, may_together: columns that a workgroup takes at once
+  // where there is much to do, and at most
+  u32 page_shift, group, q_tiles, columns, rows, together, may_together;
+  u32 fill;
 };
 typedef Arg<AttendArg> Attend;
 
@@ -126,46 +127,83 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 s) {
 // workgroups of a column.  So all of them have the same to do whatever the lengths are, and a row is in as many parts as
 // shares reach into it.
 //
-// A workgroup takes one column, its four waves every fourth tile, or `together` of them, as many waves as that leaves to each:
-// where the heads of a token lie side by side, one head's keys are 128 or 256 bytes at every n_heads-th place, and memory
-// gives less of them than of the four heads' as one piece (TB/s, 4,096 tokens a row, 8 heads: 128 rows in 8 bits 4.8 alone,
-// 64 rows in 16 bits 5.8).  It takes enough tiles that a wave has kFew of them to itself.
+// A workgroup takes one column, its four waves every fourth tile, or two or four columns, as many waves as that leaves to
+// each.  Where there is much to do it takes four (with less of it two) if the heads of a token lie side by side: one head's
+// keys are 128 or 256 bytes at every n_heads-th place, and memory gives less of them than of four heads' as one piece (8 heads,
+// 4,096 tokens a row: 128 rows in 8 bits 222 us alone, 200 so; 64 rows in 16 bits 187 and 178; 61 rows of 1 to 8,192 tokens 75
+// alone, 70 in twos, 78 in fours, where a share is short and a row in many parts).
+//
+// Where there is little, time goes by what happens one after the other: rows of few tiles are in one part, and every row has a
+// workgroup of its own if they are enough with four columns each at most (64 rows of up to 200 tokens 17 us without, 11 with;
+// 512 rows of up to 90, which are more than workgroups, 43 and 29).
 struct Share {
   u32 begin, end, per;  // places
   u32 seq, start;       // the row at `begin`, and its own place
   u32 at, column, together;
+  u32 whole;            // tiles up to which a row is one part, its who has its first tile
 };
-constexpr u32 kFew = 16;
+constexpr u32 kMuch = 16, kSome = 8, kLittle = 5;  // tiles of a wave
+constexpr u32 kWhole = 8;                         // tiles of a row
 
-// All threads of the workgroup; s_share: 6 words of LDS.
-__device__ __forceinline__ bool find_share(const Attend& a, Share& out, u32* s_share) {
+template <typename T>
+__device__ __forceinline__ T wave_incl_most(T v) {
+  v = max(v, dpp<kShr1>(v, (T)0));
+  v = max(v, dpp<kShr2>(v, (T)0));
+  v = max(v, dpp<kShr4>(v, (T)0));
+  v = max(v, dpp<kShr8>(v, (T)0));
+  v = max(v, dpp<kOfRow, 0xa>(v, (T)0));
+  return max(v, dpp<kOfHalf, 0xc>(v, (T)0));
+}
+
+struct ShareLds {
+  u32 sum[kWaves], most[kWaves], seq, start;
+};
+
+// All threads of the workgroup.
+__device__ __forceinline__ bool find_share(const Attend& a, Share& out, ShareLds& lds) {
   const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + 255) / 256;
   const u32 s0 = tid * slice, s1 = s0 + slice < n ? s0 + slice : n;
-  u32 mine = 0, before = 0, total = 0;
+  u32 mine = 0, most = 0, before = 0, total = 0;
   if (n == 1) {
-    total = span_of(a, 0).tiles() + kEach;
+    most = span_of(a, 0).tiles();
+    total = most + kEach;
   } else {
-    for (u32 s = s0; s < s1; ++s) mine += span_of(a, s).tiles() + kEach;
+    for (u32 s = s0; s < s1; ++s) {
+      const u32 t = span_of(a, s).tiles();
+      mine += t + kEach, most = max(most, t);
+    }
     const u32 inc = wave_incl_scan(mine);
-    if (lane_id() == 63) s_share[tid >> 6] = inc;
+    most = wave_incl_most(most);
+    if (lane_id() == 63) lds.sum[tid >> 6] = inc, lds.most[tid >> 6] = most;
     __syncthreads();
     before = inc - mine;
+    most = 0;
 #pragma unroll
     for (u32 w = 0; w < kWaves; ++w) {
-      if (w < tid >> 6) before += s_share[w];
-      total += s_share[w];
+      if (w < tid >> 6) before += lds.sum[w];
+      total += lds.sum[w], most = max(most, lds.most[w]);
     }
   }
-  total = uniform(total);
-  out.together = (u64)total * a.columns >= (u64)gridDim.x * kWaves * kFew ? a.together : 1;
-  const u32 columns = a.columns / out.together, shares = gridDim.x / columns, least = kLeast + kEach;
+  total = uniform(total), most = uniform(most);
+  const u64 waves = (u64)gridDim.x * kWaves, tiles = (u64)(total - n * kEach) * a.columns;
+  const bool much = tiles >= waves * kMuch, little = tiles < waves * kLittle;
+  out.together = much ? a.together : tiles >= waves * kSome && a.together > 1 ? 2 : 1;
+  u32 columns = a.columns / out.together, shares = gridDim.x / columns;
+  if (little)
+    while (n > shares && out.together < a.may_together) out.together *= 2, columns /= 2, shares *= 2;
   out.at = blockIdx.x / columns, out.column = blockIdx.x % columns * out.together;
-  out.per = (total - 1) / shares + 1;
-  if (out.per < least) out.per = least;
+  out.whole = little ? kWhole : 0;
+  out.seq = 0, out.start = 0;
+  if (little && n <= shares && most <= kWhole) {  // a row each
+    out.seq = out.at, out.per = 1;
+    out.begin = 0, out.end = kEach + 1;
+    return out.at < n;
+  }
+  const u32 least = kWaves / out.together + kEach;
+  out.per = max((total - 1) / shares + 1, least);
   if (out.at >= shares || (u64)out.at * out.per >= total) return false;
   out.begin = out.at * out.per;
   out.end = total - out.begin > out.per ? out.begin + out.per : total;
-  out.seq = 0, out.start = 0;
   if (n == 1) return true;
   if (out.begin >= before && out.begin < before + mine) {
     u32 s = s0;
@@ -174,10 +212,10 @@ __device__ __forceinline__ bool find_share(const Attend& a, Share& out, u32* s_s
       if (out.begin < before + cost) break;
       before += cost;
     }
-    s_share[4] = s, s_share[5] = before;
+    lds.seq = s, lds.start = before;
   }
   __syncthreads();
-  out.seq = uniform(s_share[4]), out.start = uniform(s_share[5]);
+  out.seq = uniform(lds.seq), out.start = uniform(lds.start);
   return true;
 }
 
@@ -387,7 +425,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
   constexpr int kWide = Tl::kWide, kParts = Tl::kParts, kSteps = Tl::kSteps, kPad = kDim + 4;
   __shared__ alignas(16) float s_o[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  __shared__ u32 s_share[6];
+  __shared__ ShareLds s_share;
   __shared__ u32 s_last;
 
   Share share;
@@ -396,7 +434,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
   const u32 wave = threadIdx.x >> 6, turn = uniform(wave / together), column = uniform(share.column + wave % together);
   const u32 head = column / a.q_tiles, q0 = column % a.q_tiles * 16;
   const u32 D = a.d.kv.head_dim, quads = D / 4, part_size = part_floats(a.rows, D);
-  const auto parts = buffer(a.parts, gridDim.x * a.together * 2 * part_size * 4);  // within 2^30 bytes
+  const auto parts = buffer(a.parts, gridDim.x * a.may_together * 2 * part_size * 4);  // within 2^30 bytes
   // the factor of the scores, made positive (its sign goes to the queries; where it is 0 they are 0, too), so that the largest
   // score is the one of the largest product and masked ones stay minus infinity
   const float factor = a.d.scale * (kF8 && a.d.kv.k_scale ? a.d.kv.k_scale[head] : 1.f) * kLog2e;
@@ -414,7 +452,11 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
     bool bad = span.bad;
     next = start + all;
     // the tiles of the row that lie in the share; a row of none is its who has the row's first place
-    const u32 lo = start > share.begin ? start : share.begin, hi = next < share.end ? next : share.end;
+    u32 lo = start > share.begin ? start : share.begin, hi = next < share.end ? next : share.end;
+    if (all && all <= share.whole) {
+      if (start < share.begin || start >= share.end) continue;
+      lo = start, hi = next;
+    }
     if (all ? lo >= hi : first_place < share.begin) continue;
     const u32 tile0 = span.first / kTile, begin = tile0 + lo - start, end = all ? tile0 + hi - start : begin;
     const bool whole = !all || (lo == start && hi == next);
@@ -630,7 +672,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
 u32 blocks_of(const Attend& a) {
   u64 shares = kCus * resident((int)a.d.kv.head_dim) / a.columns;
   const u64 places = (u64)a.d.n_seqs * ((((u64)a.d.row_pages << a.page_shift) + kTile - 1) / kTile + 1 + kEach);
-  const u64 most = (places + kLeast + kEach - 1) / (kLeast + kEach);
+  const u64 most = places / (kWaves + kEach) + 1 + a.d.n_seqs;
   if (shares > most) shares = most;
   return (u32)(shares < 1 ? 1 : shares) * a.columns;
 }
@@ -673,9 +715,10 @@ void lay_out(const fdy_attend& d, Attend& a) {
   a.q_tiles = (a.group + 15) / 16;
   a.columns = d.kv.n_heads * a.q_tiles;
   a.rows = a.group < 16 ? a.group : 16;
+  a.may_together = a.columns % 4 == 0 ? 4 : a.columns % 2 == 0 ? 2 : 1;
   // heads that lie side by side in a token, and query heads of one cache head, go together
   const bool beside = d.kv.head_stride < d.kv.token_stride || a.q_tiles > 1;
-  a.together = !beside ? 1 : a.columns % 4 == 0 ? 4 : a.columns % 2 == 0 ? 2 : 1;
+  a.together = beside ? a.may_together : 1;
 }
 size_t counter_bytes(const Attend& a) { return ((size_t)a.d.n_seqs * a.columns * 4 + 255) / 256 * 256; }
 
@@ -685,7 +728,7 @@ extern "C" size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h) {
   if (!h || !sizes_valid(*h)) return 0;
   Attend a{};
   lay_out(*h, a);
-  const size_t parts = (size_t)blocks_of(a) * a.together * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
+  const size_t parts = (size_t)blocks_of(a) * a.may_together * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
   return counter_bytes(a) + (parts + 255) / 256 * 256;
 }
 
