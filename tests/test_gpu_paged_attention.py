@@ -109,8 +109,7 @@ def check(*args, **kw):
     got = p.run()
     assert got[2] == 0
     near(got, p.want(), p.kind)
-    columns = p.H * -(-(p.q.shape[1] // p.H) // 16)
-    assert bool((p.ws[: len(p.lens) * columns * 4] == 0).all())  # counters, one a row and 16 heads of a group, are left at zero
+    assert bool((p.ws[: len(p.lens) * p.H * 4] == 0).all())  # the counters, one a row and cache head at least, are left at zero
     return p, got
 
 
@@ -132,6 +131,12 @@ def test_head_sizes_that_are_odd_multiples_of_8(D):
 def test_groups(Hq, H):
     check([5, 100, 0, 333], Hq, H, 64)
     check([290], Hq, H, 128, cache="f8", order="head")
+
+
+@pytest.mark.parametrize("Hq,H,D,cache", [(20, 1, 256, "bf16"), (20, 1, 256, "f8"), (33, 1, 128, "bf16"), (64, 2, 96, "f8"), (24, 1, 80, "bf16")])
+def test_groups_over_long_and_small_pages(Hq, H, D, cache):
+    check([2500, 17, 0, 700], Hq, H, D, cache=cache)
+    check([600, 17], Hq, H, D, cache=cache, pt=8)
 
 
 @pytest.mark.parametrize("order", ["token", "head"])
