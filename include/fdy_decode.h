@@ -12,7 +12,7 @@
  *     stays right while the sequences grow;
  *   - nothing is read back to the host, nothing is allocated, no memory is cleared by a memset.
  *
- * The conventions of fdy.h hold: d_* / device pointers inside the descriptors are the caller's, descriptors are HOST
+ * The conventions of fdy.h on memory, streams and errors hold (its integers do not: these work on floats): d_* / device pointers inside the descriptors are the caller's, descriptors are HOST
  * structs that are read during the call only, calls only enqueue, return codes and status bits are those of fdy.h.  What
  * only the device can see (a length, a page number, a row number out of range) raises FDY_ST_BAD_INDEX and is skipped as
  * stated at each call.  Unless stated otherwise arrays that a call writes do not overlap arrays that it reads.
@@ -147,7 +147,8 @@ int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stre
  *   workspace  device, 256-byte aligned, fdy_paged_attention_workspace_bytes() (0: a field out of range).  The caller
  *              clears it once, before its first use; every call leaves what it needs cleared cleared.  Calls that share one
  *              must not overlap in time, and after FDY_ERR_HIP it is cleared again.  One sized for a descriptor serves
- *              every one with no more sequences, no wider tables and the same heads, head_dim and page_tokens. */
+ *              every one with no more sequences, no wider tables and the same heads, head_dim, page_tokens and kv.type, in
+ *              any order. */
 typedef struct {
   const void* q;        /* [n_seqs][n_q_heads][head_dim] */
   void* out;            /* [n_seqs][n_q_heads][head_dim] */

@@ -27,7 +27,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 struct AttendArg {
   fdy_attend d;
   u32* status;
-  u32* counters;  // [n_seqs][columns], zero between calls
+  u32* counters;  // [shares][columns], zero between calls; a row in parts has its first share's
   float* parts;   // [shares][columns][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
   // columns: cache heads x q_tiles; rows: query heads of a tile; together, may_together: columns that a workgroup takes at once
   // where there is much to do, and at most
@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has arrived where all workgroups see it
     __syncthreads();
     if (threadIdx.x == 0) {
-      u32* counter = a.counters + (u64)seq * a.columns + share.column;
+      u32* counter = a.counters + first * a.columns + share.column;  // no other row goes on from that share to the next
       const u32 before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       s_last = before == n_parts - 1;
       if (s_last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -772,7 +772,12 @@ void lay_out(const fdy_attend& d, Attend& a) {
   const bool beside = d.kv.head_stride < d.kv.token_stride || a.q_tiles > 1;
   a.together = beside ? a.may_together : 1;
 }
-size_t counter_bytes(const Attend& a) { return ((size_t)a.d.n_seqs * a.columns * 4 + 255) / 256 * 256; }
+// For as many shares as there can be, so that it does not depend on the rows: calls for more and for fewer find their counters at
+// the same place, and neither's parts there.
+size_t counter_bytes(const Attend& a) {
+  const size_t blocks = a.columns > kCus * 2 ? a.columns : kCus * 2;
+  return (blocks * a.may_together * 4 + 255) / 256 * 256;
+}
 
 }  // namespace
 

@@ -168,6 +168,20 @@ def test_many_rows():
     check(lens, 2, 1, 64)
 
 
+@pytest.mark.parametrize("Hq,H,D,cache", [(8, 2, 64, "bf16"), (16, 4, 128, "f8"), (5, 1, 256, "bf16")])
+def test_batches_of_many_sizes_in_turn_over_one_workspace(Hq, H, D, cache):
+    rng = np.random.default_rng(5)
+    batches = [[int(x) for x in rng.integers(0, 500, 96)] + [2800, 1900], [2500, 17], [3000], [600, 0, 900, 1500, 40], [9] * 40]
+    problems = [Problem(lens, Hq, H, D, cache=cache, row_pages=200) for lens in batches]
+    ws = torch.zeros(fdd.fdy_paged_attention_workspace_bytes(problems[0].desc()), dtype=torch.uint8, device=DEV)
+    wants = [p.want() for p in problems]
+    for i in [0, 1, 0, 2, 3, 0, 4, 1, 3, 0]:
+        p = problems[i]
+        p.ws = ws
+        near(p.run(), wants[i], p.kind)
+        assert p.ws is ws  # it was wide enough
+
+
 def test_table_far_wider_than_the_rows():
     check([40, 700], 4, 2, 64, row_pages=5000)
 
