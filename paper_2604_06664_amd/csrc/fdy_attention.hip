@@ -139,6 +139,7 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 s) {
 struct Share {
   u32 begin, end, per;  // places
   u32 seq, start;       // the row at `begin`, and its own place
+  u32 seq_end;          // rows that there are for the share, for a row of no tiles does not reach a share's end
   u32 at, column, together;
   u32 whole;            // tiles up to which a row is one part, its who has its first tile
 };
@@ -193,9 +194,9 @@ __device__ __forceinline__ bool find_share(const Attend& a, Share& out, ShareLds
     while (n > shares && out.together < a.may_together) out.together *= 2, columns /= 2, shares *= 2;
   out.at = blockIdx.x / columns, out.column = blockIdx.x % columns * out.together;
   out.whole = little ? kWhole : 0;
-  out.seq = 0, out.start = 0;
+  out.seq = 0, out.start = 0, out.seq_end = n;
   if (little && n <= shares && most <= kWhole) {  // a row each
-    out.seq = out.at, out.per = 1;
+    out.seq = out.at, out.seq_end = out.at + 1, out.per = 1;
     out.begin = 0, out.end = kEach + 1;
     return out.at < n;
   }
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
   Tl::lanes(a, head, z);
 
   u32 next = share.start;
-  for (u32 seq = share.seq; next < share.end; ++seq) {
+  for (u32 seq = share.seq; seq < share.seq_end && next < share.end; ++seq) {
     const u32 first_place = next, start = next + kEach;  // places of the row, and of its first tile
     Span span = span_of(a, seq);
     span.first = uniform(span.first), span.end = uniform(span.end), span.row = uniform(span.row);

@@ -182,6 +182,17 @@ def test_batches_of_many_sizes_in_turn_over_one_workspace(Hq, H, D, cache):
         assert p.ws is ws  # it was wide enough
 
 
+@pytest.mark.parametrize("lens", [[40, 0, 0], [0, 0, 0, 0], [0, 0], [300, 9, 0, 0, 0, 0, 0]])
+@pytest.mark.parametrize("n", [1, 2])
+def test_nothing_behind_the_last_sequence_is_written(lens, n):
+    p = Problem(lens, 4, 2, 64)  # only the first n are asked for; rows behind them are empty, as the last asked for may be
+    out, lse = p.d["out"], p.d["lse"]
+    p.run(q=p.d["q"][:n], out=out[:n], lse=lse[:n])
+    o, l = p.want()[:2]
+    assert torch.equal(lse.cpu()[:n] == -math.inf, l[:n] == -math.inf)
+    assert bool((out[n:] == 5).all()) and bool((lse[n:] == 5).all())
+
+
 def test_table_far_wider_than_the_rows():
     check([40, 700], 4, 2, 64, row_pages=5000)
 
