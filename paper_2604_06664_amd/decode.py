@@ -77,6 +77,19 @@ def type_of(tensor):
     return {"torch.bfloat16": FDY_BF16, "torch.float16": FDY_F16, "torch.float8_e4m3fn": FDY_F8}[str(tensor.dtype)]
 
 
+def _want(name, x, types, shape):
+    """The kernels know of an array only its address: a tensor of another type, shape or order is refused here."""
+    if x is None or not hasattr(x, "is_contiguous"):  # a plain address is the caller's word
+        return
+    if str(x.dtype) not in [f"torch.{t}" for t in types] or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        raise ValueError(f"{name}: {types[0]} {list(shape)}, contiguous, is wanted, not {x.dtype} {list(x.shape)}")
+
+
+def _heads(name, x, like, shape):
+    if x.dtype != like.dtype or tuple(x.shape) != tuple(shape) or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError(f"{name}: {like.dtype} {list(shape)} with contiguous last dimension is wanted, not {x.dtype} {list(x.shape)}")
+
+
 def make_rope(rot_dim, base=10000.0, scaling=FDY_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, trained_len=4096.0,
               magnitude=1.0):
     return fdy_rope(scaling, rot_dim, base, factor, low, high, trained_len, magnitude)
@@ -92,15 +105,19 @@ def make_kv(k, v, *, type, n_pages, page_tokens, n_heads, head_dim, page_stride,
 def make_append_desc(*, q, k, v, q_out, positions, table, kv, rot_dim, slots=None, k_out=None, layout=FDY_ROPE_HALF):
     """q, k, v, q_out, k_out: tensors [tokens, heads, dim] with contiguous last dimension; table [positions, 2, rot_dim / 2]."""
     d = fdy_append()
-    for name, x in (("q", q), ("k", k), ("v", v), ("q_out", q_out), ("k_out", k_out)):
+    n, keys = k.shape[0], (k.shape[0], kv.n_heads, kv.head_dim)
+    queries = None if q is None else (n, q.shape[1], kv.head_dim)
+    for name, x, shape in (("q", q, queries), ("k", k, keys), ("v", v, keys), ("q_out", q_out, queries), ("k_out", k_out, keys)):
         setattr(d, name, _ptr(x))
         if x is not None:
-            if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
-                raise ValueError(f"{name}: [tokens, heads, dim] with contiguous last dimension is wanted")
+            _heads(name, x, k, shape or keys)
             setattr(d, name + "_token", x.stride(0))
             setattr(d, name + "_head", x.stride(1))
+    _want("positions", positions, ["int32"], (n,))
+    _want("table", table, ["float32"], (table.shape[0], 2, rot_dim // 2))
+    _want("slots", slots, ["int64"], (n,))
     d.positions, d.table, d.slots = _ptr(positions), _ptr(table), _ptr(slots)
-    d.kv, d.n_tokens, d.n_q_heads = kv, k.shape[0], 0 if q is None else q.shape[1]
+    d.kv, d.n_tokens, d.n_q_heads = kv, n, 0 if q is None else q.shape[1]
     d.n_positions, d.rot_dim, d.type, d.layout = table.shape[0], rot_dim, type_of(k), layout
     return d
 
@@ -108,8 +125,11 @@ def make_append_desc(*, q, k, v, q_out, positions, table, kv, rot_dim, slots=Non
 def make_attend_desc(*, q, out, table, lens, kv, scale, lse=None, rows=None, window=0):
     """q, out: tensors [sequences, heads, dim] with contiguous last dimension; table [rows, pages] and lens, 32-bit."""
     for name, x in (("q", q), ("out", out)):
-        if x.dim() != 3 or x.stride(2) != 1:
-            raise ValueError(f"{name}: [sequences, heads, dim] with contiguous last dimension is wanted")
+        _heads(name, x, q, (q.shape[0], q.shape[1], kv.head_dim))
+    _want("table", table, ["int32"], table.shape[:2])
+    _want("lens", lens, ["int32"], table.shape[:1])
+    _want("rows", rows, ["int32"], q.shape[:1])
+    _want("lse", lse, ["float32"], q.shape[:2])
     d = fdy_attend(_ptr(q), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), _ptr(rows), q.stride(0), q.stride(1),
                    out.stride(0), out.stride(1), kv, scale, window, q.shape[0], q.shape[1], table.shape[0],
                    table.shape[1], type_of(q), 0)
@@ -118,6 +138,11 @@ def make_attend_desc(*, q, out, table, lens, kv, scale, lse=None, rows=None, win
 
 def make_pages(*, refs, free_bits, table, lens, page_tokens, planes=None, page_bytes=0, page_stride=0):
     """refs [pages], table [rows, pages of a row], lens [rows], 32-bit; free_bits, planes (device addresses) 64-bit."""
+    _want("refs", refs, ["int32", "uint32"], refs.shape[:1])
+    _want("free_bits", free_bits, ["int64", "uint64"], ((refs.shape[0] + 63) // 64,))
+    _want("table", table, ["int32"], table.shape[:2])
+    _want("lens", lens, ["int32"], table.shape[:1])
+    _want("planes", planes, ["int64", "uint64"], () if planes is None else planes.shape[:1])
     return fdy_pages(_ptr(refs), _ptr(free_bits), _ptr(table), _ptr(lens), _ptr(planes), page_bytes, page_stride,
                      refs.shape[0], page_tokens, table.shape[0], table.shape[1], 0 if planes is None else planes.shape[0], 0)
 

@@ -182,3 +182,56 @@ def test_lists_of_nothing_are_fine():
     assert fdd.fdy_pages_free(d, None, 0, None, **k) == FDY_OK
     assert fdd.fdy_pages_copy(d, None, None, 0, None, **k) == FDY_OK
     assert fdd.fdy_pages_copy(pages(n_planes=0), A, A, 3, None, **k) == FDY_OK
+
+
+class Meta:
+    """Tensors that own nothing, of a kind that each helper takes; a wrong one is refused."""
+
+    @staticmethod
+    def of(shape, dtype="float32"):
+        torch = pytest.importorskip("torch")
+        return torch.empty(shape, dtype=getattr(torch, dtype), device="meta")
+
+    def append(self, **kw):
+        x = lambda h: self.of((3, h, 64), "bfloat16")  # noqa: E731
+        args = dict(q=x(4), k=x(2), v=x(2), q_out=x(4), k_out=x(2), positions=self.of(3, "int32"), table=self.of((9, 2, 16)),
+                    slots=self.of(3, "int64"), kv=kv(n_heads=2, head_dim=64), rot_dim=32)
+        return fdd.make_append_desc(**{**args, **kw})
+
+    def attend(self, **kw):
+        x = self.of((3, 4, 64), "bfloat16")
+        args = dict(q=x, out=x, lse=self.of((3, 4)), table=self.of((5, 7), "int32"), lens=self.of(5, "int32"),
+                    rows=self.of(3, "int32"), kv=kv(n_heads=2, head_dim=64), scale=1.0)
+        return fdd.make_attend_desc(**{**args, **kw})
+
+    def pages(self, **kw):
+        args = dict(refs=self.of(70, "int32"), free_bits=self.of(2, "int64"), table=self.of((5, 7), "int32"),
+                    lens=self.of(5, "int32"), page_tokens=16, planes=self.of(3, "int64"))
+        return fdd.make_pages(**{**args, **kw})
+
+
+@pytest.mark.parametrize("helper,wrong", [
+    ("append", dict(q=((3, 4, 64), "float16"))), ("append", dict(q=((2, 4, 64), "bfloat16"))), ("append", dict(k=((3, 1, 64), "bfloat16"))),
+    ("append", dict(v=((3, 2, 32), "bfloat16"))), ("append", dict(q_out=((3, 2, 64), "bfloat16"))), ("append", dict(k_out=((3, 128), "bfloat16"))),
+    ("append", dict(positions=((3,), "int64"))), ("append", dict(positions=((4,), "int32"))), ("append", dict(slots=((3,), "int32"))),
+    ("append", dict(table=((9, 2, 32), "float32"))), ("append", dict(table=((9, 2, 16), "float64"))),
+    ("attend", dict(q=((3, 4, 32), "bfloat16"))), ("attend", dict(out=((3, 2, 64), "bfloat16"))), ("attend", dict(out=((3, 4, 64), "float32"))),
+    ("attend", dict(table=((5, 7), "int64"))), ("attend", dict(lens=((5,), "int64"))), ("attend", dict(lens=((4,), "int32"))),
+    ("attend", dict(rows=((5,), "int32"))), ("attend", dict(lse=((3, 4), "bfloat16"))), ("attend", dict(lse=((4, 3), "float32"))),
+    ("pages", dict(refs=((70,), "int64"))), ("pages", dict(free_bits=((1,), "int64"))), ("pages", dict(free_bits=((2,), "int32"))),
+    ("pages", dict(table=((5, 7), "int64"))), ("pages", dict(lens=((7,), "int32"))), ("pages", dict(planes=((3,), "int32")))])
+def test_helpers_refuse_other_types_and_shapes(helper, wrong):
+    make = getattr(Meta(), helper)
+    make()
+    with pytest.raises(ValueError):
+        make(**{name: Meta.of(*x) for name, x in wrong.items()})
+
+
+def test_helpers_refuse_other_orders():
+    m = Meta()
+    with pytest.raises(ValueError):
+        m.attend(table=m.of((7, 5), "int32").t())
+    with pytest.raises(ValueError):
+        m.attend(q=m.of((3, 64, 4), "bfloat16").transpose(1, 2))
+    with pytest.raises(ValueError):
+        m.append(k=m.of((3, 64, 2), "bfloat16").transpose(1, 2))
