@@ -12,7 +12,7 @@
 //                 the same eight tokens of one element of v in a lane: the lane loads eight tokens by eight elements and
 //                 transposes them in registers (v_perm).
 // A query head's maximum, sum and output all lie in one lane column, so rescaling needs no exchange but the maximum over the
-// four groups.  Four waves take the tiles of a piece in turn and join in LDS; the pieces of a row are joined by whichever
+// four groups.  Four or eight waves take the tiles of a piece in turn and join in LDS; the pieces of a row are joined by whichever
 // workgroup finishes last.
 #include "fdy_types.hpp"
 
@@ -20,7 +20,7 @@ using namespace fdy;
 
 namespace {
 
-constexpr u32 kWaves = 4, kTile = 32, kCus = 256;
+constexpr u32 kTile = 32, kCus = 256;
 constexpr u32 kEach = 3;  // what a row costs beside its tiles (queries, join, output), in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -32,7 +32,7 @@ struct AttendArg {
   // columns: cache heads x q_tiles; rows: query heads of a tile; together, may_together: columns that a workgroup takes at once
   // where there is much to do, and at most
   u32 page_shift, group, q_tiles, columns, rows, together, may_together;
-  u32 fill;
+  u32 eight;  // waves of a workgroup are eight, not four
 };
 typedef Arg<AttendArg> Attend;
 
@@ -127,7 +127,7 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 s) {
 // workgroups of a column.  So all of them have the same to do whatever the lengths are, and a row is in as many parts as
 // shares reach into it.
 //
-// A workgroup takes one column, its four waves every fourth tile, or two or four columns, as many waves as that leaves to
+// A workgroup takes one column, its waves every fourth or eighth tile, or two or four columns, as many waves as that leaves to
 // each.  Where there is much to do it takes four (with less of it two) if the heads of a token lie side by side: one head's
 // keys are 128 or 256 bytes at every n_heads-th place, and memory gives less of them than of four heads' as one piece (8 heads,
 // 4,096 tokens a row: 128 rows in 8 bits 222 us alone, 200 so; 64 rows in 16 bits 187 and 178; 61 rows of 1 to 8,192 tokens 75
@@ -156,13 +156,16 @@ __device__ __forceinline__ T wave_incl_most(T v) {
   return max(v, dpp<kOfHalf, 0xc>(v, (T)0));
 }
 
+template <u32 kWaves>
 struct ShareLds {
   u32 sum[kWaves], most[kWaves], seq, start;
 };
 
 // All threads of the workgroup.
-__device__ __forceinline__ bool find_share(const Attend& a, Share& out, ShareLds& lds) {
-  const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + 255) / 256;
+template <u32 kWaves>
+__device__ __forceinline__ bool find_share(const Attend& a, Share& out, ShareLds<kWaves>& lds) {
+  constexpr u32 kThreads = 64 * kWaves;
+  const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + kThreads - 1) / kThreads;
   const u32 s0 = tid * slice, s1 = s0 + slice < n ? s0 + slice : n;
   u32 mine = 0, most = 0, before = 0, total = 0;
   if (n == 1) {
@@ -416,22 +419,25 @@ struct Tile {
 // Workgroups of a compute unit that are launched, and that the registers leave room for.  More do not help: of rows of 4,096
 // tokens in 8 bits, three give 4.6 TB/s where two give 5.1; and one more of 128 elements in 16 bits leaves 168 registers and
 // a few spills, whose reloads wait behind all keys and values under way (2.1 TB/s).
-constexpr u32 resident(int dim) { return dim <= 128 ? 2 : 1; }
+//
+// Eight waves of one workgroup do the work of two workgroups of four in half as many parts and with less of a tail, as all waves
+// of a compute unit end together (see `lay_out`); of 256 elements four waves have all the registers, and are alone.
+constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; }
 
 // kTiles: tiles of 16 query heads a workgroup, for one read of their keys and values (64 rows of 8,192 tokens, 32 heads of one
 // cache head: of 128 elements 77 us with a workgroup for each 16, 73 so; of 64 elements, two cache heads, 81 and 66.  What is
 // left above the read is the parts' 16 KiB a workgroup, written through to memory by all at once).
-template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles>
-__global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
+template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves>
+__global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_kernel(Attend a) {
   typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
   constexpr int kWide = Tl::kWide, kParts = Tl::kParts, kSteps = Tl::kSteps, kPad = kDim + 4;
-  constexpr u32 kRows = 16 * kTiles;
+  constexpr u32 kRows = 16 * kTiles, kThreads = 64 * kWaves;
   constexpr int kPair = kTiles == 2 && (kF8 || kDim <= 64) ? 2 : 1;  // (128 elements in 16 bits would spill)
   __shared__ alignas(16) float s_o[kWaves][kRows][kPad];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
-  __shared__ ShareLds s_share;
+  __shared__ ShareLds<kWaves> s_share;
   __shared__ u32 s_last;
 
   Share share;
@@ -603,7 +609,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
     auto part_at = [&](u32 share_no, u32 c, bool second) {
       return ((share_no * a.columns + share.column + c) * 2 + second) * part_size;
     };
-    for (u32 i = threadIdx.x; i < items; i += 256) {
+    for (u32 i = threadIdx.x; i < items; i += kThreads) {
       const Item it = item(i);
       if (!it.there) continue;
       float M = -INFINITY;
@@ -644,8 +650,8 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
     const bool second = start > first * share.per;
     // `crews` of threads take every crews-th part each, or kPair items at once where there are more than threads, eight parts'
     // loads of each under way: what comes from another die takes microseconds
-    const u32 crews = items >= 256 ? 1 : 256 / items;
-    for (u32 i0 = 0; i0 < items; i0 += 256 * kPair) {
+    const u32 crews = items >= kThreads ? 1 : kThreads / items;
+    for (u32 i0 = 0; i0 < items; i0 += kThreads * kPair) {
       const u32 crew = crews > 1 ? threadIdx.x / items : 0, i = i0 + threadIdx.x - crew * items;
       Item it[kPair];
       bool works[kPair];
@@ -653,7 +659,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
       f32x4 x[kPair];
 #pragma unroll
       for (int g = 0; g < kPair; ++g) {
-        it[g] = item(i + 256 * g);
+        it[g] = item(i + kThreads * g);
         works[g] = it[g].there && (g ? crews == 1 : crew < crews);
         M[g] = -INFINITY, L[g] = 0.f, x[g] = 0;
       }
@@ -690,7 +696,7 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
       }
       if (crews > 1) {  // the crews' sums, in their order
         float(*c_x)[4] = (float(*)[4])s_o;
-        float(*c_ml)[2] = (float(*)[2])(c_x + 256);
+        float(*c_ml)[2] = (float(*)[2])(c_x + kThreads);
         if (works[0]) *(f32x4*)c_x[threadIdx.x] = x[0], c_ml[threadIdx.x][0] = M[0], c_ml[threadIdx.x][1] = L[0];
         __syncthreads();
         if (works[0] && crew == 0) {
@@ -716,26 +722,33 @@ __global__ void __launch_bounds__(256, resident(kDim)) attend_kernel(Attend a) {
 
 // As many workgroups as are resident together, fewer where the longest rows that the table allows have not the tiles; a
 // multiple of the columns.
-u32 blocks_of(const Attend& a) {
-  u64 shares = kCus * resident((int)a.d.kv.head_dim) / a.columns;
-  const u64 places = (u64)a.d.n_seqs * ((((u64)a.d.row_pages << a.page_shift) + kTile - 1) / kTile + 1 + kEach);
-  const u64 most = places / (kWaves + kEach) + 1 + a.d.n_seqs;
+u64 row_tiles(const fdy_attend& d) { return ((u64)d.row_pages * d.kv.page_tokens + kTile - 1) / kTile; }
+u32 blocks_of(const Attend& a, u32 waves) {
+  u64 shares = kCus * resident((int)a.d.kv.head_dim, waves) / a.columns;
+  const u64 places = a.d.n_seqs * (row_tiles(a.d) + 1 + kEach);
+  const u64 most = places / (waves + kEach) + 1 + a.d.n_seqs;
   if (shares > most) shares = most;
   return (u32)(shares < 1 ? 1 : shares) * a.columns;
 }
 
 template <typename T, bool kF8, int kDim>
 int launch_attend(const Attend& a, hipStream_t stream) {
-  const u32 blocks = blocks_of(a);
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, stream, a); };
-  constexpr int kTwo = kDim <= 128 || kF8 ? 2 : 1;
+  auto go = [&](auto kernel, u32 waves) {
+    hipLaunchKernelGGL(kernel, dim3(blocks_of(a, waves)), dim3(64 * waves), 0, stream, a);
+  };
+  constexpr int kTwo = kDim <= 128 || kF8 ? 2 : 1, kOnce = kNonTemporal;
+  constexpr u32 kMost = kDim <= 128 ? 8 : 4;
   if (a.d.kv.page_tokens < 16)
-    go(attend_kernel<T, kF8, kDim, true, 0, 1>);
+    go(attend_kernel<T, kF8, kDim, true, 0, 1, 4>, 4);
+  else if (a.eight && a.q_tiles == 1)
+    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, kOnce, kTwo, kMost>, kMost) : go(attend_kernel<T, kF8, kDim, false, kOnce, 1, kMost>, kMost);
+  else if (a.eight)
+    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, 0, kTwo, kMost>, kMost) : go(attend_kernel<T, kF8, kDim, false, 0, 1, kMost>, kMost);
   else if (a.q_tiles == 1)
-    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, kNonTemporal, kTwo>) : go(attend_kernel<T, kF8, kDim, false, kNonTemporal, 1>);
+    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, kOnce, kTwo, 4>, 4) : go(attend_kernel<T, kF8, kDim, false, kOnce, 1, 4>, 4);
   else
-    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, 0, kTwo>) : go(attend_kernel<T, kF8, kDim, false, 0, 1>);
+    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, 0, kTwo, 4>, 4) : go(attend_kernel<T, kF8, kDim, false, 0, 1, 4>, 4);
   FDY_HIP_TRY(hipGetLastError());
   return FDY_OK;
 }
@@ -772,6 +785,13 @@ void lay_out(const fdy_attend& d, Attend& a) {
   // heads that lie side by side in a token, and query heads of one cache head, go together
   const bool beside = d.kv.head_stride < d.kv.token_stride || a.q_tiles > 1;
   a.together = beside ? a.may_together : 1;
+  // Eight waves a workgroup where the tables allow much (the lengths are not known here) and a token's heads lie together: 64 rows
+  // of 1,024 tokens 48 us, with four 58; 128 of 4,096 in 8 bits 176 and 206; 32 of 512 18 and 23; 8 of 8,192 with one cache head
+  // 35 and 57.  Four where it is little (8 rows of 300 to 900 tokens 15, with eight 19; 64 of 20 to 200 11 and 13) or the heads
+  // lie apart (64 of 4,096 160 and 165)
+  const u64 tiles = row_tiles(d), all = tiles * d.n_seqs * a.columns, waves = kCus * 8;
+  a.eight = d.kv.head_dim <= 128 && d.kv.page_tokens >= 16 && (d.kv.head_stride <= d.kv.token_stride || a.q_tiles > 1) &&
+            (tiles >= 256 || (tiles >= 16 && all >= waves * 2));
 }
 // For as many shares as there can be, so that it does not depend on the rows: calls for more and for fewer find their counters at
 // the same place, and neither's parts there.
@@ -786,7 +806,8 @@ extern "C" size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h) {
   if (!h || !sizes_valid(*h)) return 0;
   Attend a{};
   lay_out(*h, a);
-  const size_t parts = (size_t)blocks_of(a) * a.may_together * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
+  // (four waves' workgroups, which are more: a call for fewer rows or narrower tables may take these)
+  const size_t parts = (size_t)blocks_of(a, 4) * a.may_together * 2 * part_floats(a.rows, h->kv.head_dim) * 4;
   return counter_bytes(a) + (parts + 255) / 256 * 256;
 }
 

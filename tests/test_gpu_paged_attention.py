@@ -193,6 +193,40 @@ def test_nothing_behind_the_last_sequence_is_written(lens, n):
     assert bool((out[n:] == 5).all()) and bool((lse[n:] == 5).all())
 
 
+WIDE = 8192 // 16  # pages of a table that allows long rows, whatever their lengths are
+
+
+@pytest.mark.parametrize("lens", [EDGES, [2500, 17, 0, 700], [5, 0, 9, 0], [3000], [1, 2, 3] * 90 + [0]])
+@pytest.mark.parametrize("D,kind,cache", [(128, "bf16", "bf16"), (128, "f16", "f8"), (64, "f16", "f16"), (80, "bf16", "bf16"), (48, "bf16", "f8")])
+def test_tables_that_allow_long_rows(lens, D, kind, cache):
+    check(lens, 8, 4, D, kind=kind, cache=cache, row_pages=WIDE)
+    check(lens[:6], 3, 1, D, kind=kind, cache=cache, row_pages=WIDE, order="head")
+
+
+@pytest.mark.parametrize("Hq,H", [(1, 1), (16, 1), (32, 1), (40, 1), (64, 2), (33, 3), (100, 1), (24, 8)])
+@pytest.mark.parametrize("D,cache", [(64, "bf16"), (128, "f8"), (128, "bf16")])
+def test_groups_in_tables_that_allow_long_rows(Hq, H, D, cache):
+    p, got = check([1900, 0, 333, 64, 2100], Hq, H, D, cache=cache, row_pages=WIDE, sharp=2.0)
+    again = p.run()  # the same every time, over the same workspace
+    assert torch.equal(again[0].view(torch.int16), got[0].view(torch.int16)) and torch.equal(again[1], got[1])
+
+
+def test_windows_in_tables_that_allow_long_rows():
+    for window in (1, 33, 500):
+        check([0, 1, 64, 333, 1520, 2000], 4, 2, 128, row_pages=WIDE, window=window, first_tokens_gone=True)
+
+
+def test_wide_and_narrow_tables_in_turn_over_one_workspace():
+    wide = Problem([900, 5, 2400, 31], 8, 4, 128, row_pages=WIDE)
+    narrow = Problem([900, 5, 2400, 31], 8, 4, 128)
+    few = Problem([4], 8, 4, 128)
+    ws = torch.zeros(fdd.fdy_paged_attention_workspace_bytes(wide.desc()), dtype=torch.uint8, device=DEV)
+    for p in (wide, narrow, wide, few, narrow, few, wide):
+        p.ws = ws
+        near(p.run(), p.want(), "bf16")
+        assert p.ws is ws
+
+
 def test_table_far_wider_than_the_rows():
     check([40, 700], 4, 2, 64, row_pages=5000)
 
