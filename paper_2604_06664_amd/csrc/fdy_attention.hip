@@ -130,8 +130,8 @@ __device__ __forceinline__ Span span_of(const Attend& a, u32 s) {
 // A workgroup takes one column, its waves every fourth or eighth tile, or two or four columns, as many waves as that leaves to
 // each.  Where there is much to do it takes four (with less of it two) if the heads of a token lie side by side: one head's
 // keys are 128 or 256 bytes at every n_heads-th place, and memory gives less of them than of four heads' as one piece (8 heads,
-// 4,096 tokens a row: 128 rows in 8 bits 222 us alone, 200 so; 64 rows in 16 bits 187 and 178; 61 rows of 1 to 8,192 tokens 75
-// alone, 70 in twos, 78 in fours, where a share is short and a row in many parts).
+// 4,096 tokens a row: 128 rows in 8 bits 231 us alone, 193 in twos, 177 in fours; 64 rows in 16 bits 191, 173 and 171; 16 rows
+// 58 alone and 53 in twos; 33 rows of 1,024 and 256 elements 49, 46 and, in fours, where a share is short and a row in many parts, 51).
 //
 // Where there is little, time goes by what happens one after the other: rows of few tiles are in one part, and every row has a
 // workgroup of its own if they are enough with four columns each at most (64 rows of up to 200 tokens 17 us without, 11 with;
@@ -143,7 +143,7 @@ struct Share {
   u32 at, column, together;
   u32 whole;            // tiles up to which a row is one part, its who has its first tile
 };
-constexpr u32 kMuch = 16, kSome = 8, kLittle = 5;  // tiles of a wave
+constexpr u32 kMuch = 16, kSome = 2, kLittle = 5;  // tiles of a wave
 constexpr u32 kWhole = 8;                         // tiles of a row
 
 template <typename T>
