@@ -421,7 +421,7 @@ struct Tile {
 // a few spills, whose reloads wait behind all keys and values under way (2.1 TB/s).
 //
 // Eight waves of one workgroup do the work of two workgroups of four in half as many parts and with less of a tail, as all waves
-// of a compute unit end together (see `lay_out`); of 256 elements four waves have all the registers, and are alone.
+// of a compute unit end together (see `lay_out`).  Of 256 elements in 16 bits four waves have all the registers, and are alone.
 constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; }
 
 // kTiles: tiles of 16 query heads a workgroup, for one read of their keys and values (64 rows of 8,192 tokens, 32 heads of one
@@ -738,13 +738,13 @@ int launch_attend(const Attend& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3(blocks_of(a, waves)), dim3(64 * waves), 0, stream, a);
   };
   constexpr int kTwo = kDim <= 128 || kF8 ? 2 : 1, kOnce = kNonTemporal;
-  constexpr u32 kMost = kDim <= 128 ? 8 : 4;
+  constexpr u32 kMost = kDim <= 128 || kF8 ? 8 : 4, kMostTwo = kDim <= 128 ? 8 : 4;
   if (a.d.kv.page_tokens < 16)
     go(attend_kernel<T, kF8, kDim, true, 0, 1, 4>, 4);
   else if (a.eight && a.q_tiles == 1)
-    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, kOnce, kTwo, kMost>, kMost) : go(attend_kernel<T, kF8, kDim, false, kOnce, 1, kMost>, kMost);
+    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, kOnce, kTwo, kMostTwo>, kMostTwo) : go(attend_kernel<T, kF8, kDim, false, kOnce, 1, kMost>, kMost);
   else if (a.eight)
-    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, 0, kTwo, kMost>, kMost) : go(attend_kernel<T, kF8, kDim, false, 0, 1, kMost>, kMost);
+    a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, 0, kTwo, kMostTwo>, kMostTwo) : go(attend_kernel<T, kF8, kDim, false, 0, 1, kMost>, kMost);
   else if (a.q_tiles == 1)
     a.rows > 16 ? go(attend_kernel<T, kF8, kDim, false, kOnce, kTwo, 4>, 4) : go(attend_kernel<T, kF8, kDim, false, kOnce, 1, 4>, 4);
   else
@@ -788,10 +788,10 @@ void lay_out(const fdy_attend& d, Attend& a) {
   // Eight waves a workgroup where the tables allow much (the lengths are not known here) and a token's heads lie together: 64 rows
   // of 1,024 tokens 48 us, with four 58; 128 of 4,096 in 8 bits 176 and 206; 32 of 512 18 and 23; 8 of 8,192 with one cache head
   // 35 and 57.  Four where it is little (8 rows of 300 to 900 tokens 15, with eight 19; 64 of 20 to 200 11 and 13) or the heads
-  // lie apart (64 of 4,096 160 and 165)
+  // lie apart (64 of 4,096 160 and 165); of 256 elements eight are too many for the registers in 16 bits, for LDS with 32 query heads
   const u64 tiles = row_tiles(d), all = tiles * d.n_seqs * a.columns, waves = kCus * 8;
-  a.eight = d.kv.head_dim <= 128 && d.kv.page_tokens >= 16 && (d.kv.head_stride <= d.kv.token_stride || a.q_tiles > 1) &&
-            (tiles >= 256 || (tiles >= 16 && all >= waves * 2));
+  a.eight = (d.kv.head_dim <= 128 || (d.kv.type == FDY_F8 && a.rows <= 16)) && d.kv.page_tokens >= 16 &&
+            (d.kv.head_stride <= d.kv.token_stride || a.q_tiles > 1) && (tiles >= 256 || (tiles >= 16 && all >= waves * 2));
 }
 // For as many shares as there can be, so that it does not depend on the rows: calls for more and for fewer find their counters at
 // the same place, and neither's parts there.

@@ -211,6 +211,13 @@ def test_groups_in_tables_that_allow_long_rows(Hq, H, D, cache):
     assert torch.equal(again[0].view(torch.int16), got[0].view(torch.int16)) and torch.equal(again[1], got[1])
 
 
+@pytest.mark.parametrize("Hq,H", [(8, 4), (16, 1), (20, 1), (3, 1)])
+def test_wide_heads_of_8_bits_in_tables_that_allow_long_rows(Hq, H):
+    for D in (192, 256):
+        check([1900, 0, 333, 64, 2100, 31], Hq, H, D, cache="f8", row_pages=WIDE)
+        check([9, 0, 100, 0], Hq, H, D, cache="f8", row_pages=WIDE)
+
+
 def test_windows_in_tables_that_allow_long_rows():
     for window in (1, 33, 500):
         check([0, 1, 64, 333, 1520, 2000], 4, 2, 128, row_pages=WIDE, window=window, first_tokens_gone=True)
