@@ -1,7 +1,7 @@
 // fdy_attention.hip - attention of one new token of every sequence over its pages, split over the length and joined.
 //
 // out = sum_t e^(x_t) v_t / sum_t e^(x_t), x_t = scale k_t.q, in one pass over the keys and values with a running maximum
-// and sum.  All query heads of a cache head read the same keys and values, 2 * group flops a byte: the bound is memory, and
+// and sum.  All query heads of a cache head read the same keys and values, a flop a byte each (two in 8 bits): the bound is memory, and
 // the matrix cores only keep the arithmetic out of its way (a tile holds 16 query heads of a cache head, a wave one or two of them).
 //
 // A wave takes 32 tokens at a time, straight from the pages into the operands, no LDS in the loop:
@@ -417,7 +417,7 @@ struct Tile {
 
 // ---- the kernel -----------------------------------------------------------------------------------------
 // Workgroups of a compute unit that are launched, and that the registers leave room for.  More do not help: of rows of 4,096
-// tokens in 8 bits, three give 4.6 TB/s where two give 5.1; and one more of 128 elements in 16 bits leaves 168 registers and
+// tokens in 8 bits, three of four waves give 4.6 TB/s where two give 5.1; and one more of 128 elements in 16 bits leaves 168 registers and
 // a few spills, whose reloads wait behind all keys and values under way (2.1 TB/s).
 //
 // Eight waves of one workgroup do the work of two workgroups of four in half as many parts and with less of a tail, as all waves
@@ -425,8 +425,8 @@ struct Tile {
 constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; }
 
 // kTiles: tiles of 16 query heads a workgroup, for one read of their keys and values (64 rows of 8,192 tokens, 32 heads of one
-// cache head: of 128 elements 77 us with a workgroup for each 16, 73 so; of 64 elements, two cache heads, 81 and 66.  What is
-// left above the read is the parts' 16 KiB a workgroup, written through to memory by all at once).
+// cache head, workgroups of four waves: of 128 elements 77 us with one for each 16, 73 so; of 64 elements, two cache heads, 81 and 66;
+// with eight waves 62 and 58.  What is left above the read is the parts' 16 KiB a workgroup, written through to memory by all at once).
 template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves>
 __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_kernel(Attend a) {
   typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
@@ -775,7 +775,7 @@ void lay_out(const fdy_attend& d, Attend& a) {
   a.page_shift = log2_of(d.kv.page_tokens);
   a.group = d.n_q_heads / d.kv.n_heads;
   // 32 query heads of a cache head go together; 16 where their sums would not fit the registers, where pages are small, or where
-  // tiles of 16 are fewer (40 heads of one, 64 rows of 4,096 tokens in 8 bits: 61 us, and 74 as two times 20)
+  // tiles of 16 are fewer (40 heads of one, 64 rows of 4,096 tokens in 8 bits, four waves: 61 us, and 74 as two times 20)
   const bool two = d.kv.page_tokens >= 16 && (d.kv.head_dim <= 128 || d.kv.type == FDY_F8) && (a.group + 31) / 32 * 2 == (a.group + 15) / 16;
   const u32 rows = two ? 32 : 16;
   a.q_tiles = (a.group + rows - 1) / rows;
