@@ -216,3 +216,23 @@ def test_another_stream_and_replays():
             close(qo[t].cpu(), y, size, "bf16")
             s = int(slots[t])
             assert torch.equal(vp[s // pt, s % pt], v[t])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "f8"])
+def test_cache_offsets_behind_32_bits(cache):
+    T, H, D, pt, stride = 3, 2, 64, 16, (1 << 32) + 4096  # elements from page 0 to page 1
+    rng = np.random.default_rng(7)
+    k, v = (torch.from_numpy(rng.standard_normal((T, H, D)).astype(np.float32)).to(torch.bfloat16).to(DEV) for _ in "kv")
+    pools = [torch.empty(stride + pt * H * D, dtype=DTYPES[cache], device=DEV) for _ in "kv"]
+    kv = fdd.make_kv(*pools, type=fdd.TYPES[cache], n_pages=2, page_tokens=pt, n_heads=H, head_dim=D, page_stride=stride,
+                     token_stride=H * D, head_stride=D)
+    place = [0, pt - 1, 5]
+    slots = torch.tensor([pt + p for p in place], dtype=torch.int64, device=DEV)
+    pos = torch.tensor([2, 7, 0], dtype=torch.int32, device=DEV)
+    table = table_of(D, 8)
+    fdd.fdy_rope_append(fdd.make_append_desc(q=None, k=k, v=v, q_out=None, positions=pos, table=table, kv=kv, rot_dim=D, slots=slots))
+    got_k, got_v = (p[stride:].view(pt, H, D)[place].cpu() for p in pools)
+    for t in range(T):
+        y, size = od.turned(k[t].cpu().double(), table[int(pos[t])].cpu(), D, "half")
+        close(got_k[t], y, size, cache)
+        close(got_v[t], v[t].cpu().double(), v[t].cpu().double().abs(), cache)
