@@ -535,14 +535,15 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
           float mx = y[0];
 #pragma unroll
           for (int j = 1; j < 8; ++j) mx = fmaxf(mx, y[j]);
-          mx = over_groups(mx, larger) * scale;
-          const float m_new = fmaxf(m[qt], mx), ref = m_new == -INFINITY ? 0.f : m_new;
-          keep[qt] = __builtin_amdgcn_exp2f(m[qt] - ref);
+          // The maximum is kept of the products, and the factor is applied to differences from it: the largest weight is
+          // 1 whatever the size of the scores.  (Of scores of 2^30 and more the rounding of `product * factor` is worth e^64.)
+          const float m_new = fmaxf(m[qt], over_groups(mx, larger)), ref = m_new == -INFINITY ? 0.f : m_new;
+          keep[qt] = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
           m[qt] = m_new;
           float part = 0.f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j], scale, -ref));
+            const float e = __builtin_amdgcn_exp2f((y[j] - ref) * scale);
             part += e;
             p[qt][j] = (elem)e;
           }
@@ -579,7 +580,7 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
 #pragma unroll
           for (int e = 0; e < kWide; ++e)
             s_o[wave][qt * 16 + z.col][pt * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[qt][pt * kWide + e][i];
-      if (z.grp == 0) s_m[wave][qt * 16 + z.col] = m[qt], s_l[wave][qt * 16 + z.col] = sum[qt];
+      if (z.grp == 0) s_m[wave][qt * 16 + z.col] = m[qt] * scale, s_l[wave][qt * 16 + z.col] = sum[qt];
     }
     __syncthreads();
     // item i: four elements (from 4 qd on) of query head r of column c of the workgroup's

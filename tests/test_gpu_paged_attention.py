@@ -382,3 +382,49 @@ def test_no_sequences():
     fdd.fdy_paged_attention(d, None, 0)
     torch.cuda.synchronize()
     assert bool((p.d["out"] == 5).all())
+
+
+def put(p, which, values):
+    """values [row][token, head, dim] in the place of the rows' keys (0) or values (1), on both sides."""
+    view = p.views[which].clone().contiguous()
+    for r, x in enumerate(values):
+        for t in range(x.shape[0]):
+            view[p.table[r, t // p.pt], t % p.pt] = x[t].to(view.dtype)
+    p.views[which] = view
+    p.pools[which].copy_(view.view(torch.uint8 if p.cache == "f8" else torch.int16).flatten())
+
+
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "f8"), ("f16", "f8")])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_size(kind, cache, sign):
+    """Scores of 2^20 to 2^30 (2^60 with bf16), which are not more than a few bits of 32: the largest, of one token or of three,
+    take all the weight, and the weight is theirs in full.  Each score is one exact product, so nothing but the rounding of
+    weights and result is allowed: 1 or 1/3 of at most 4."""
+    lens, most = [40, 300, 3000, 1], 30 if kind == "f16" else 60
+    p = Problem(lens, 8, 2, 64, kind=kind, cache=cache, scale=sign * 1.75, seed=21)
+    rng = np.random.default_rng(22)
+    wide = 8 if cache == "f8" else 15 if kind == "f16" else 30  # bits of the largest key
+    sizes = np.linspace(20, most, 8) - wide
+    # keys of a few bits, three of them or one the largest; queries with some bits of their own
+    q = torch.zeros_like(p.q)
+    q[:, :, 0] = torch.from_numpy(2.0 ** np.minimum(sizes, 15 if kind == "f16" else 100) * rng.uniform(1, 1.9, (4, 8))).to(q.dtype)
+    p.q = q
+    p.d["q"].copy_(q)
+    keys = []
+    for n in lens:
+        k = torch.zeros(n, 2, 64)
+        k[:, :, 0] = torch.from_numpy(rng.integers(-6, 6, (n, 2)).astype(np.float32)) * 2.0 ** (wide - 4)
+        for h in range(2):
+            k[rng.permutation(n)[:3 if h else 1], h, 0] = 7.0 * 2.0 ** (wide - 4)
+        keys.append(k * sign)
+    put(p, 0, keys)
+    if p.scales[0] is not None:
+        for s, d in zip(p.scales, p.d["scales"]):
+            s.copy_(torch.tensor([0.5, 2.0]))  # products stay exact
+            d.copy_(s)
+    out, lse, status = p.run()
+    assert status == 0
+    o, l, spread = p.want()
+    u = ROUND[kind]
+    assert bool(((out.double() - o).abs() <= 2 * u * spread[..., None]).all()), float((out.double() - o).abs().max())
+    assert bool(((lse.double() - l).abs() <= l.abs() * 2.0 ** -21 + 1e-6).all())
