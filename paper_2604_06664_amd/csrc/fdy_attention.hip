@@ -24,6 +24,14 @@ constexpr u32 kTile = 32, kCus = 256;
 constexpr u32 kEach = 3;  // what a row costs beside its tiles (queries, join, output), in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// Weights e^(x - max) are at most 1.  In f16 they would be held in steps of 2^-24 below 2^-14, and at 2^-25 be gone, which many
+// small ones beside a large one together are not: there they are held 2^15 times as large (as are their sum and the output until
+// the division), with all 11 bits down to 2^-29.
+template <typename T>
+constexpr float kLift = 0.f;
+template <>
+constexpr float kLift<F16> = 15.f;
+
 struct AttendArg {
   fdy_attend d;
   u32* status;
@@ -536,14 +544,14 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
 #pragma unroll
           for (int j = 1; j < 8; ++j) mx = fmaxf(mx, y[j]);
           // The maximum is kept of the products, and the factor is applied to differences from it: the largest weight is
-          // 1 whatever the size of the scores.  (Of scores of 2^30 and more the rounding of `product * factor` is worth e^64.)
+          // 1 (2^15 in f16) whatever the size of the scores.  (Of scores of 2^30 and more the rounding of `product * factor` is worth e^64.)
           const float m_new = fmaxf(m[qt], over_groups(mx, larger)), ref = m_new == -INFINITY ? 0.f : m_new;
           keep[qt] = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
           m[qt] = m_new;
           float part = 0.f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float e = __builtin_amdgcn_exp2f((y[j] - ref) * scale);
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j] - ref, scale, kLift<T>));
             part += e;
             p[qt][j] = (elem)e;
           }
@@ -580,7 +588,7 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
 #pragma unroll
           for (int e = 0; e < kWide; ++e)
             s_o[wave][qt * 16 + z.col][pt * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[qt][pt * kWide + e][i];
-      if (z.grp == 0) s_m[wave][qt * 16 + z.col] = m[qt] * scale, s_l[wave][qt * 16 + z.col] = sum[qt];
+      if (z.grp == 0) s_m[wave][qt * 16 + z.col] = m[qt] * scale - kLift<T>, s_l[wave][qt * 16 + z.col] = sum[qt];
     }
     __syncthreads();
     // item i: four elements (from 4 qd on) of query head r of column c of the workgroup's

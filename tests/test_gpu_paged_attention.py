@@ -428,3 +428,41 @@ def test_scores_of_any_size(kind, cache, sign):
     u = ROUND[kind]
     assert bool(((out.double() - o).abs() <= 2 * u * spread[..., None]).all()), float((out.double() - o).abs().max())
     assert bool(((lse.double() - l).abs() <= l.abs() * 2.0 ** -21 + 1e-6).all())
+
+
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f16"), ("f16", "f8")])
+@pytest.mark.parametrize("pt", [4, 16])
+def test_many_small_weights_beside_large_ones(kind, cache, pt):
+    """In every 32 tokens one takes nearly all the weight and has the value 0; what comes out is of the others, whose scores are
+    up to 20 below.  Relative to the result: one rounding of a weight to the type and one of the result (in f16 half the smallest
+    step, 2^-25, where that is more), and 2^-13 for scores of this size and the exponential.  (Heads differ in how far below.)"""
+    lens = [33, 300, 2111, 64]
+    p = Problem(lens, 8, 2, 64, kind=kind, cache=cache, pt=pt, scale=1.0, seed=31)
+    rng = np.random.default_rng(32)
+    q = torch.zeros_like(p.q)
+    q[:, :, 0] = torch.tensor([10.0, 14.0, 15.5, 16.5, 17.0, 17.5, 18.0, 20.0]).to(q.dtype)
+    p.q = q
+    p.d["q"].copy_(q)
+    keys, values = [], []
+    for n in lens:
+        k, v = torch.zeros(n, 2, 64), torch.from_numpy(rng.uniform(100, 400, (n, 2, 64)).astype(np.float32)) * (1 if cache == "f8" else 16)
+        k[:, :, 0] = -1.0
+        for t in range(0, n, 32):
+            at = t + int(rng.integers(0, min(32, n - t)))
+            k[at], v[at] = 0.0, 0.0
+        keys.append(k)
+        values.append(v)
+    put(p, 0, keys)
+    put(p, 1, values)
+    for s, d in zip(p.scales, p.d["scales"]):
+        if s is not None:
+            s.copy_(torch.tensor([1.0, 1.0]))
+            d.copy_(s)
+    out, lse, status = p.run()
+    assert status == 0
+    o, l, _ = p.want()
+    u = ROUND[kind]
+    seen = o != 0
+    err = ((out.double() - o).abs() - (2.0 ** -25 if kind == "f16" else 0))[seen] / o[seen]
+    assert float(err.max()) <= 2 * u + 2.0 ** -13, float(err.max())
+    assert bool(((lse.double() - l).abs() <= 3e-5).all())
