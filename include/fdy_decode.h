@@ -135,8 +135,8 @@ int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stre
  *   x_t = scale * q_h . k_t            over t in [max(0, n - window), n)     (window 0: all)
  *   out_h = sum_t e^(x_t) v_t / sum_t e^(x_t),   lse_h = ln sum_t e^(x_t)
  * No tokens (or all x_t minus infinity): out 0, lse minus infinity.  Products are of the stored types (F8 widened
- * exactly), sums, maxima and the joining of parts are held in 32 bits; e^(x_t - max) is rounded to `type` (to all of its
- * significant bits, however small against the largest down to 2^-29) for its product with v, out once at the end.  What lies in pages behind the row's length is not read.
+ * exactly), sums, maxima and the joining of parts are held in 32 bits; e^(x_t - max) goes as two elements of `type`
+ * into its product with v (2^-15 of it is lost with bf16, 2^-21 with f16; of one below 2^-18 with f16 2^-40), out once at the end.  What lies in pages behind the row's length is not read.
  *   lens outside [0, row_pages * page_tokens]: held within, FDY_ST_BAD_INDEX; rows outside [0, n_rows): as no tokens, and
  *   FDY_ST_BAD_INDEX; a page number outside [0, kv.n_pages): its tokens are left out, FDY_ST_BAD_INDEX.
  * The results do not depend on what else is in the batch except in the rounding of joined parts, and are the same every

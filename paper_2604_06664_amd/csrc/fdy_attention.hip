@@ -75,6 +75,32 @@ __device__ __forceinline__ u32 widen_f8x2<F16, true>(u32 w) {
   return __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true));
 }
 
+// A product with v takes weights of its own type only, 8 bits of bf16 and 11 of f16, which is all that the outputs have: so each
+// goes as two, the first rounded down to one step below, the rest (of one to two steps) as the second: 2^-15 of a weight is lost, or 2^-21.
+// The rest is not 0 where the weight is not, for an infinite value times 0 would be no number.  The second product costs nothing
+// where memory bounds the call (64 rows of 4,096 tokens 171 us with and without), 1 or 2 % in 8 bits (64 of 4,096 tokens, 40 heads of
+// one: 60 for 59).
+template <typename T>
+__device__ __forceinline__ void split(float x, float y, u32& first, u32& rest);
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32 step_below(u32 pair) {
+  return __builtin_bit_cast(u32, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, pair), (u16x2)(1)));
+}
+template <>
+__device__ __forceinline__ void split<Bf16>(float x, float y, u32& first, u32& rest) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  first = step_below(__builtin_amdgcn_perm(__builtin_bit_cast(u32, y), __builtin_bit_cast(u32, x), 0x07060302u));
+  const bf16x2 r = {(__bf16)(x - __builtin_bit_cast(float, first << 16)), (__bf16)(y - __builtin_bit_cast(float, first & 0xffff0000u))};
+  rest = __builtin_bit_cast(u32, r);
+}
+template <>
+__device__ __forceinline__ void split<F16>(float x, float y, u32& first, u32& rest) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  first = step_below(__builtin_bit_cast(u32, __builtin_amdgcn_cvt_pkrtz(x, y)));
+  const f16x2 f = __builtin_bit_cast(f16x2, first), r = {(_Float16)(x - (float)f[0]), (_Float16)(y - (float)f[1])};
+  rest = __builtin_bit_cast(u32, r);
+}
+
 // Largest / sum over the four lanes that differ in l / 16: a swap of halves, then of rows, of a value with itself.  (The
 // results are taken out of their vector first: hipcc 7.2 casts element 0 whichever element of a vector it is handed.)
 __device__ __forceinline__ float over_groups(float x, float (*op)(float, float)) {
@@ -533,7 +559,7 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
         bool seen[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) seen[j] = x.seen(a, z, span, ids, t, j / 4, j % 4);
-        x8 p[kTiles];
+        x8 p[kTiles], rest[kTiles];
         float keep[kTiles];
 #pragma unroll
         for (int qt = 0; qt < kTiles; ++qt) {
@@ -549,12 +575,17 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
           keep[qt] = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
           m[qt] = m_new;
           float part = 0.f;
+          v4u32 first_of, rest_of;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j] - ref, scale, kLift<T>));
-            part += e;
-            p[qt][j] = (elem)e;
+          for (int j = 0; j < 4; ++j) {
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(y[2 * j] - ref, scale, kLift<T>));
+            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(y[2 * j + 1] - ref, scale, kLift<T>));
+            part += e0 + e1;
+            u32 a, b;
+            split<T>(e0, e1, a, b);
+            first_of[j] = a, rest_of[j] = b;
           }
+          p[qt] = __builtin_bit_cast(x8, first_of), rest[qt] = __builtin_bit_cast(x8, rest_of);
           sum[qt] = sum[qt] * keep[qt] + part;
         }
 #pragma unroll
@@ -569,6 +600,8 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
               f32x4& c1 = o[qt][pt * kWide + 2 * e2 + 1];
               c0 = mfma<T>(even, p[qt], c0 * keep[qt]);
               c1 = mfma<T>(odd, p[qt], c1 * keep[qt]);
+              c0 = mfma<T>(even, rest[qt], c0);
+              c1 = mfma<T>(odd, rest[qt], c1);
             }
           }
         x.load_v(a, z, span, ids_next, t_next, bad);

@@ -466,3 +466,36 @@ def test_many_small_weights_beside_large_ones(kind, cache, pt):
     err = ((out.double() - o).abs() - (2.0 ** -25 if kind == "f16" else 0))[seen] / o[seen]
     assert float(err.max()) <= 2 * u + 2.0 ** -13, float(err.max())
     assert bool(((lse.double() - l).abs() <= 3e-5).all())
+
+
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "f8")])
+@pytest.mark.parametrize("group", [4, 32])
+def test_weights_are_held_in_more_bits_than_the_type_has(kind, cache, group):
+    """One token of 32 takes most of the weight and has the value 0, all others have one and the same score and the value 1, so
+    a rounding of the weights would not average out.  Products are exact; 2^-15 is left to the weights, 2^-16 to factor,
+    exponential and sums, and the result is rounded once."""
+    lens = [33, 64, 300, 2111]
+    p = Problem(lens, 2 * group, 2, 128, kind=kind, cache=cache, scale=1.0, seed=41)
+    q = torch.zeros_like(p.q)
+    q[:, :, 0] = torch.linspace(1.5, 7.5, 4 * 2 * group).view(4, -1).to(q.dtype)
+    p.q = q
+    p.d["q"].copy_(q)
+    keys, values = [], []
+    for n in lens:
+        k, v = torch.zeros(n, 2, 128), torch.ones(n, 2, 128)
+        k[:, :, 0] = -1.0
+        k[5::32], v[5::32] = 0.0, 0.0
+        keys.append(k)
+        values.append(v)
+    put(p, 0, keys)
+    put(p, 1, values)
+    for s, d in zip(p.scales, p.d["scales"]):
+        if s is not None:
+            s.copy_(torch.tensor([1.0, 1.0]))
+            d.copy_(s)
+    out, lse, status = p.run()
+    assert status == 0
+    o, l, _ = p.want()
+    err = float(((out.double() - o).abs() / o).max())
+    assert err <= ROUND[kind] + 2.0 ** -15 + 2.0 ** -16, err
+    assert bool(((lse.double() - l).abs() <= 3e-5).all())
