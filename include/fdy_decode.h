@@ -136,7 +136,8 @@ int fdy_rope_append(const fdy_append* h_desc, uint32_t* d_status, void* hip_stre
  *   out_h = sum_t e^(x_t) v_t / sum_t e^(x_t),   lse_h = ln sum_t e^(x_t)
  * No tokens (or all x_t minus infinity): out 0, lse minus infinity.  Products are of the stored types (F8 widened
  * exactly), sums, maxima and the joining of parts are held in 32 bits; e^(x_t - max) goes as two elements of `type`
- * into its product with v (2^-15 of it is lost with bf16, 2^-21 with f16; of one below 2^-18 with f16 2^-40), out once at the end.  What lies in pages behind the row's length is not read.
+ * into its product with v (2^-15 of it is lost with bf16, 2^-21 with f16; of one below 2^-18 with f16 2^-40), out is rounded
+ * once at the end.  What lies in pages behind the row's length is not read.
  *   lens outside [0, row_pages * page_tokens]: held within, FDY_ST_BAD_INDEX; rows outside [0, n_rows): as no tokens, and
  *   FDY_ST_BAD_INDEX; a page number outside [0, kv.n_pages): its tokens are left out, FDY_ST_BAD_INDEX.
  * The results do not depend on what else is in the batch except in the rounding of joined parts, and are the same every
@@ -208,8 +209,9 @@ size_t fdy_pages_workspace_bytes(const fdy_pages* h_pages, uint32_t n);
  * copied first, in all planes, to a page of the row's own; of rows that hold such a page among themselves alone the last in
  * the list keeps it.
  *   A row gets all or nothing: one that does not fit its table, or whose pages the pool has not left after all rows before
- *   it (those that get nothing for want of pages count as well), or whose tokens end behind n_slots, stays as it is, its
- *   slots are -1 (positions as if), and FDY_ST_CAPACITY is raised.
+ *   it (those that get nothing for want of pages count as well), or that would keep a page of which one of these still holds
+ *   the other share, or whose tokens end behind n_slots, stays as it is, its slots are -1 (positions as if), and
+ *   FDY_ST_CAPACITY is raised.
  *   counts[i] < 0 counts as 0 and raises FDY_ST_BAD_INDEX.  n <= 65,536; the sum of counts < 2^31. */
 int fdy_pages_extend(const fdy_pages* h_pages, const int32_t* d_rows, const int32_t* d_counts, uint32_t n,
                      int64_t* d_slots, int32_t* d_positions, uint32_t n_slots, void* d_workspace, size_t workspace_bytes,

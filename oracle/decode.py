@@ -154,20 +154,27 @@ class Books:
             last.append(p)
             if p >= 0 and self.refs[p] > 1:
                 asks.setdefault(p, []).append(i)
-        copies = [False] * n
+        copies, others = [False] * n, [[] for _ in rows]
         for p, who in asks.items():
-            for i in who[:-1] if len(who) == self.refs[p] else who:
+            keeps = len(who) == self.refs[p]
+            for i in who[:-1] if keeps else who:
                 copies[i] = True
+            if keeps:
+                others[who[-1]] = who[:-1]
         need = [(self.pages_of(self.lens[r] + counts[i]) - self.pages_of(self.lens[r]) + copies[i]) if fits[i] else 0
                 for i, r in enumerate(rows)]
         free = [p for p, c in enumerate(self.refs) if c == 0]
         slots, positions = [], []
-        taken, moved = 0, []
+        taken, moved, got = 0, [], []
         for i, r in enumerate(rows):
             served = fits[i]
             if served and need[i] and taken + need[i] > len(free):
                 self.status |= ST_CAPACITY
                 served = False
+            if served and not all(got[j] for j in others[i]):  # the page that it would keep is still another's as well
+                self.status |= ST_CAPACITY
+                served = False
+            got.append(served)
             mine = free[taken:taken + need[i]]
             taken += need[i]
             old = self.lens[r] if good[i] else 0

@@ -114,6 +114,7 @@ __device__ __forceinline__ ExtendWords extend_layout(const Pages& a) {
 // What an entry of the list wants, and its pages' first number among those found.
 struct Entry {
   u32 row, count, length, last, need, rank;
+  u32 others;  // of one that keeps a shared page: up to which number of found pages the others' copies of it go, where pages are short
   bool copies, fits;
 };
 
@@ -122,7 +123,8 @@ template <typename Taken>
 __device__ __forceinline__ void serve(const Pages& a, const ExtendWords& w, u32 i, const Entry& e, u32 found, Taken taken,
                                       u32* s_served, u32& wrong) {
   bool served = e.fits;
-  if (served && e.need && (u64)e.rank + e.need > found) wrong |= FDY_ST_CAPACITY, served = false;
+  // (one that keeps a page takes none, but the page is not its own as long as another has not got its copy)
+  if (served && ((e.need && (u64)e.rank + e.need > found) || e.others > found)) wrong |= FDY_ST_CAPACITY, served = false;
   u32 copy = kNoPage;
   int32_t* table = a.d.table + (u64)(served ? e.row : 0) * a.d.row_pages;
   u32 at_end = kNoPage;  // page of the first new token
@@ -240,10 +242,19 @@ __global__ void __launch_bounds__(kBooksThreads) extend_books_kernel(Pages a) {
     for (; bits && rank < total; bits &= bits - 1) w.taken[rank++] = (w0 + tid) * 64 + (u32)__builtin_ctzll(bits);
   }
   if (found > total) found = total;
+  auto keeps = [&](u32 i) { return w.last[i] != kNoPage && !(w.need[i] & kCopies); };
+  if (found < total) {
+    for (u32 i = tid; i < a.n; i += kBooksThreads)
+      if (keeps(i)) w.asked[w.last[i]] = 0;
+    __syncthreads();
+    for (u32 i = tid; i < a.n; i += kBooksThreads)
+      if (w.need[i] & kCopies) atomicMax(w.asked + w.last[i], w.rank[i] + (w.need[i] & ~kCopies));
+  }
   __syncthreads();
   // the rows that get theirs
   for (u32 i = tid; i < a.n; i += kBooksThreads) {
     Entry e;
+    e.others = found < total && keeps(i) ? fresh(w.asked + w.last[i]) : 0;
     e.row = row_of(i), e.count = a.to ? (u32)a.to[i] : 1u, e.length = w.length[i] & ~kUnserved, e.last = w.last[i];
     e.need = w.need[i] & ~kCopies, e.rank = w.rank[i], e.copies = w.need[i] & kCopies, e.fits = !(w.length[i] & kUnserved);
     serve(a, w, i, e, (u32)found, [&](u32 r) { return w.taken[r]; }, &s_served, wrong);
@@ -343,6 +354,14 @@ __global__ void __launch_bounds__(kBooksThreads) extend_few_kernel(Pages a) {
     }
   }
   if (found > total) found = total;
+  if (found < total) {
+    const bool keeps = shared && !e.copies;
+    if (keeps) s_pages.sum[page_at] = 0;
+    __syncthreads();
+    if (e.copies) atomicMax(&s_pages.sum[page_at], e.rank + e.need);
+    __syncthreads();
+    if (keeps) e.others = s_pages.sum[page_at];
+  }
   __syncthreads();
   const auto taken = [&](u32 r) { return r < kTakenHere ? s_taken[r] : w.taken[r]; };
   if (there) {

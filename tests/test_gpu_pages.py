@@ -334,3 +334,37 @@ def test_replays():
         p.want.free([10])
         p.same()
         assert slots.cpu().tolist() == s.tolist() and pos.cpu().tolist() == q.tolist()
+
+
+@pytest.mark.parametrize("more", [0, 1500])
+def test_rows_that_keep_a_page_wait_for_the_other_holders(more):
+    """Pairs of rows of one partly filled page each, pages short: where the first of a pair gets no copy the second must not go
+    on in the page.  `more` rows behind them have room in pages of their own (long lists are kept by another kernel)."""
+    for pages_left in (0, 1, 2, 3):
+        for rows in ([0, 1, 2, 3], [2, 0, 1, 3], [1, 0, 3, 2], [3, 1, 2, 0], [0, 1], [2, 3, 1]):
+            own = list(range(4, 4 + more))
+            table = [[0, -1], [0, -1], [1, -1], [1, -1]] + [[r - 2, -1] for r in own]
+            refs = [2, 2] + [1] * more + [0] * pages_left
+            p = Pool(refs, table, [5, 5, 9, 9] + [3] * more, 16, n_planes=1)
+            p.extend(rows + own, None)
+            p.extend(list(reversed(rows)) + own, [1 + (r == 2) for r in rows] + [2] * more)
+            p.extend(own + rows, [1] * more + [12 if r == 1 else 1 for r in rows])
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_beams_in_a_pool_that_runs_out(seed):
+    rng = np.random.default_rng(200 + seed)
+    pt, beams, groups = 8, 2 + seed % 3, [6, 500][seed % 2]
+    lens = np.repeat(rng.integers(1, 3 * pt, groups), beams)
+    pages = -(-lens[::beams] // pt)
+    table, refs = np.full((groups * beams, 6), -1, int), np.zeros(int(pages.sum()) + groups * beams // 2, int)
+    order, at = rng.permutation(len(refs)), 0
+    for g, k in enumerate(pages):
+        table[g * beams:(g + 1) * beams, :k] = order[at:at + k]
+        refs[order[at:at + k]] = beams
+        at += k
+    p = Pool(refs, table, lens, pt, n_planes=1, page_bytes=16, stride=16)
+    for _ in range(4):
+        p.extend([int(r) for r in rng.permutation(len(lens))], [int(c) for c in rng.integers(0, 3, len(lens))])
+        src, dst = rng.permutation(len(lens))[:5], rng.permutation(len(lens))[:5]
+        p.fork([int(x) for x in src], [int(x) for x in dst])
