@@ -184,7 +184,7 @@ int fdy_paged_attention(const fdy_attend* h_desc, void* d_workspace, size_t work
  * be written the first counts, the others are skipped with FDY_ST_BAD_INDEX.
  *   refs, table, lens, rows 4-byte, free_bits, planes, slots 8-byte aligned; planes' addresses, page_bytes, page_stride
  *   multiples of 16, page_bytes < 2^30; page_tokens a power of two up to 65,536; n_pages, n_rows <= 2^28, row_pages <= 2^25,
- *   row_pages * page_tokens < 2^31, n_planes <= 32,768 */
+ *   row_pages * page_tokens < 2^31, n_planes <= 32,768, n_planes * ceil(page_bytes / 8,192) < 2^32 */
 typedef struct {
   uint32_t* refs;      /* [n_pages]              */
   uint64_t* free_bits; /* [ceil(n_pages / 64)]   */

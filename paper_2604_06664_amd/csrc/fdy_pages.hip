@@ -593,10 +593,11 @@ bool pages_valid(const fdy_pages& d) {
   if (d.reserved || !d.n_pages || d.n_pages > 1u << 28 || d.n_rows > 1u << 28 || d.row_pages > 1u << 25) return false;
   if (!power_of_two(d.page_tokens) || d.page_tokens > 65536u || (u64)d.row_pages * d.page_tokens >= 1ull << 31) return false;
   if (d.n_planes && (d.page_bytes % 16 || d.page_stride % 16 || d.page_bytes >> 30 || d.page_stride >> 40)) return false;
+  if (d.n_planes * ((d.page_bytes + kPiece - 1) / kPiece) >> 32) return false;  // kernels count a page's pieces in 32 bits
   return d.n_planes <= 32768u;
 }
 
-// `pages`: the call takes or gives pages; `rows`: it reads rows; `planes`: it moves contents
+// `books`: the call reads or writes the books; `planes`: it moves contents
 int check(const fdy_pages* h, bool books, bool planes) {
   if (!h || !pages_valid(*h)) return FDY_ERR_INVALID_ARG;
   if (books && (!h->refs || !h->free_bits || !aligned(h->refs, 4) || !aligned(h->free_bits, 8))) return FDY_ERR_INVALID_ARG;

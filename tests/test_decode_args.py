@@ -235,3 +235,11 @@ def test_helpers_refuse_other_orders():
         m.attend(q=m.of((3, 64, 4), "bfloat16").transpose(1, 2))
     with pytest.raises(ValueError):
         m.append(k=m.of((3, 64, 2), "bfloat16").transpose(1, 2))
+
+
+def test_pages_refuse_more_pieces_than_32_bits_count():
+    """32,768 planes of pages of 2^30 - 16 bytes are 2^32 pieces of 8 KiB: a count in 32 bits would be 0, and nothing copied."""
+    d = pages(n_planes=32768, page_bytes=(1 << 30) - 16, page_stride=1 << 30)
+    assert fdd.fdy_pages_workspace_bytes(d, 3) == 0
+    assert set(page_calls(d, ALL).values()) == {FDY_ERR_INVALID_ARG}
+    assert fdd.fdy_pages_workspace_bytes(pages(n_planes=32767, page_bytes=(1 << 30) - 16, page_stride=1 << 30), 3) > 0
