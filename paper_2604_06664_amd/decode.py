@@ -90,6 +90,21 @@ def _heads(name, x, like, shape):
         raise ValueError(f"{name}: {like.dtype} {list(shape)} with contiguous last dimension is wanted, not {x.dtype} {list(x.shape)}")
 
 
+_KV_TYPES = {FDY_BF16: "torch.bfloat16", FDY_F16: "torch.float16", FDY_F8: "torch.float8_e4m3fn"}
+
+
+def _pool(name, x, type, n_pages, page_tokens, n_heads, head_dim, page_stride, token_stride, head_stride):
+    """A pool's elements are of the cache's type (or integers, as raw storage), and its last page ends within its storage."""
+    if x is None or not hasattr(x, "untyped_storage"):
+        return
+    if (x.is_floating_point() or x.is_complex()) and str(x.dtype) != _KV_TYPES.get(type):
+        raise ValueError(f"{name}: a pool of {_KV_TYPES.get(type, 'a known type')} is wanted, not {x.dtype}")
+    last = ((n_pages - 1) * page_stride + (page_tokens - 1) * token_stride + (n_heads - 1) * head_stride + head_dim)
+    there = x.untyped_storage().nbytes() - x.storage_offset() * x.element_size()
+    if last * (1 if type == FDY_F8 else 2) > there:
+        raise ValueError(f"{name}: {n_pages} pages with these strides end behind the tensor's {there} bytes")
+
+
 def make_rope(rot_dim, base=10000.0, scaling=FDY_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, trained_len=4096.0,
               magnitude=1.0):
     return fdy_rope(scaling, rot_dim, base, factor, low, high, trained_len, magnitude)
@@ -97,7 +112,11 @@ def make_rope(rot_dim, base=10000.0, scaling=FDY_ROPE_PLAIN, factor=1.0, low=1.0
 
 def make_kv(k, v, *, type, n_pages, page_tokens, n_heads, head_dim, page_stride, token_stride, head_stride,
             k_scale=None, v_scale=None):
-    """k, v: device pools (tensors or addresses) or None; strides in elements."""
+    """k, v: device pools (tensors or addresses) or None; strides in elements; scales float32 [n_heads]."""
+    for name, x in (("k", k), ("v", v)):
+        _pool(name, x, type, n_pages, page_tokens, n_heads, head_dim, page_stride, token_stride, head_stride)
+    _want("k_scale", k_scale, ["float32"], (n_heads,))
+    _want("v_scale", v_scale, ["float32"], (n_heads,))
     return fdy_kv(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), page_stride, token_stride, head_stride, type, n_pages,
                   page_tokens, n_heads, head_dim, 0)
 

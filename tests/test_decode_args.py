@@ -243,3 +243,46 @@ def test_pages_refuse_more_pieces_than_32_bits_count():
     assert fdd.fdy_pages_workspace_bytes(d, 3) == 0
     assert set(page_calls(d, ALL).values()) == {FDY_ERR_INVALID_ARG}
     assert fdd.fdy_pages_workspace_bytes(pages(n_planes=32767, page_bytes=(1 << 30) - 16, page_stride=1 << 30), 3) > 0
+
+
+CACHE = dict(type=fdd.FDY_BF16, n_pages=4, page_tokens=16, n_heads=2, head_dim=64, page_stride=2048, token_stride=128, head_stride=64)
+
+
+@pytest.mark.parametrize("type_,dtype", [(fdd.FDY_BF16, "bfloat16"), (fdd.FDY_F16, "float16"), (fdd.FDY_F8, "float8_e4m3fn")])
+def test_caches_of_tensors(type_, dtype):
+    of, args = Meta.of, {**CACHE, "type": type_}
+    scale = of(2) if type_ == fdd.FDY_F8 else None
+    fdd.make_kv(of((4, 16, 2, 64), dtype), of((4, 16, 2, 64), dtype), k_scale=scale, v_scale=scale, **args)
+    raw = of(4 * 2048 * (1 if type_ == fdd.FDY_F8 else 2), "uint8")  # storage without a type
+    fdd.make_kv(raw, raw, **args)
+    both = of((4, 2, 16, 2, 64), dtype)  # keys and values of a page side by side: the values' last page ends with the tensor
+    fdd.make_kv(both[:, 0], both[:, 1], **{**args, "page_stride": 4096})
+    with pytest.raises(ValueError):
+        fdd.make_kv(both[:, 1], both[:, 1], **{**args, "page_stride": 4096 + 8})
+    for other in {"bfloat16", "float16", "float8_e4m3fn", "float32"} - {dtype}:
+        for pools in ((of((4, 16, 2, 64), other), of((4, 16, 2, 64), dtype)), (of((4, 16, 2, 64), dtype), of((4, 16, 2, 64), other))):
+            with pytest.raises(ValueError):
+                fdd.make_kv(*pools, **args)
+
+
+@pytest.mark.parametrize("kw", [dict(n_pages=5), dict(n_pages=9999), dict(page_stride=2056), dict(token_stride=136), dict(head_dim=128),
+                                dict(n_heads=3), dict(page_tokens=32)])
+def test_caches_behind_the_end_of_their_tensors_are_refused(kw):
+    good, short = Meta.of((5, 32, 3, 128), "bfloat16"), Meta.of((4, 16, 2, 64), "bfloat16")
+    args = {**CACHE, **kw}
+    for pools in ((good, short), (short, good)):
+        with pytest.raises(ValueError):
+            fdd.make_kv(*[p if p is short else None for p in pools], **args)
+    fdd.make_kv(A, A, **args)  # addresses are the caller's word
+
+
+@pytest.mark.parametrize("shape,dtype", [((1,), "float32"), ((), "float32"), ((3,), "float32"), ((2,), "float64"), ((2,), "bfloat16"),
+                                         ((2, 1), "float32")])
+def test_scales_of_other_types_and_shapes_are_refused(shape, dtype):
+    pool, scale = Meta.of((4, 16, 2, 64), "float8_e4m3fn"), Meta.of(2)
+    args = {**CACHE, "type": fdd.FDY_F8}
+    fdd.make_kv(pool, pool, k_scale=scale, v_scale=scale, **args)
+    for kw in (dict(k_scale=Meta.of(shape, dtype), v_scale=scale), dict(k_scale=scale, v_scale=Meta.of(shape, dtype)),
+               dict(k_scale=Meta.of((2, 2))[:, 0], v_scale=scale)):
+        with pytest.raises(ValueError):
+            fdd.make_kv(pool, pool, **kw, **args)
