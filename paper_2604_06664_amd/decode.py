@@ -5,6 +5,7 @@ taken from them; the caller keeps the tensors alive) and handed to every call.""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 from . import FDY_ERR_INVALID_ARG, FDY_ERR_WORKSPACE, FDY_OK, FdyError, _check, _ptr, _stream, lib  # noqa: F401
 
@@ -83,6 +84,19 @@ def _want(name, x, types, shape):
         return
     if str(x.dtype) not in [f"torch.{t}" for t in types] or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
         raise ValueError(f"{name}: {types[0]} {list(shape)}, contiguous, is wanted, not {x.dtype} {list(x.shape)}")
+
+
+@functools.lru_cache(maxsize=None)
+def _is(dtype, types):
+    return str(dtype) in [f"torch.{t}" for t in types]
+
+
+def _list(name, x, types, n):
+    """A tensor that a call reads or writes `n` elements of; made for every call, so short."""
+    if x is None or not hasattr(x, "is_contiguous"):
+        return
+    if not _is(x.dtype, types) or x.numel() < n or not x.is_contiguous():
+        raise ValueError(f"{name}: {types[0]}, contiguous, of {n} elements at least, is wanted, not {x.dtype} {list(x.shape)}")
 
 
 def _heads(name, x, like, shape):
@@ -166,6 +180,9 @@ def make_pages(*, refs, free_bits, table, lens, page_tokens, planes=None, page_b
                      refs.shape[0], page_tokens, table.shape[0], table.shape[1], 0 if planes is None else planes.shape[0], 0)
 
 
+_I32, _U32, _I64 = ("int32",), ("int32", "uint32"), ("int64",)
+
+
 # ---- entry points (names as in include/fdy_decode.h) --------------------------------------------
 def fdy_rope_frequencies(h_rope, check=True):
     """-> (rc, host array of rot_dim / 2 frequencies)."""
@@ -179,6 +196,7 @@ def fdy_rope_frequencies(h_rope, check=True):
 
 
 def fdy_rope_table(h_rope, first, n_positions, d_table, stream=None, check=True):
+    _list("d_table", d_table, ("float32",), 0 if h_rope is None else int(n_positions) * h_rope.rot_dim)
     rc = _L().fdy_rope_table(_d(h_rope), int(first), int(n_positions), _ptr(d_table), _stream(stream))
     return _check(rc, "fdy_rope_table") if check else rc
 
@@ -208,28 +226,38 @@ def fdy_pages_workspace_bytes(h_pages, n):
 
 def fdy_pages_extend(h_pages, d_rows, d_counts, n, d_slots, d_positions, n_slots, d_workspace, workspace_bytes,
                      d_status=None, stream=None, check=True):
+    for name, x, types, least in (("d_rows", d_rows, _I32, n), ("d_counts", d_counts, _I32, n), ("d_slots", d_slots, _I64, n_slots),
+                                  ("d_positions", d_positions, _I32, n_slots)):
+        _list(name, x, types, least)
     rc = _L().fdy_pages_extend(_d(h_pages), _ptr(d_rows), _ptr(d_counts), int(n), _ptr(d_slots), _ptr(d_positions),
                                int(n_slots), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_extend") if check else rc
 
 
 def fdy_pages_fork(h_pages, d_src, d_dst, n, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    _list("d_src", d_src, _I32, n)
+    _list("d_dst", d_dst, _I32, n)
     rc = _L().fdy_pages_fork(_d(h_pages), _ptr(d_src), _ptr(d_dst), int(n), _ptr(d_workspace), int(workspace_bytes),
                              _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_fork") if check else rc
 
 
 def fdy_pages_free(h_pages, d_rows, n, d_status=None, stream=None, check=True):
+    _list("d_rows", d_rows, _I32, n)
     rc = _L().fdy_pages_free(_d(h_pages), _ptr(d_rows), int(n), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_free") if check else rc
 
 
 def fdy_pages_copy(h_pages, d_src, d_dst, n, d_status=None, stream=None, check=True):
+    _list("d_src", d_src, _I32, n)
+    _list("d_dst", d_dst, _I32, n)
     rc = _L().fdy_pages_copy(_d(h_pages), _ptr(d_src), _ptr(d_dst), int(n), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_copy") if check else rc
 
 
 def fdy_pages_compact(h_pages, d_map, d_n_live, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    _list("d_map", d_map, _I32, 0 if h_pages is None else h_pages.n_pages)
+    _list("d_n_live", d_n_live, _U32, 1)
     rc = _L().fdy_pages_compact(_d(h_pages), _ptr(d_map), _ptr(d_n_live), _ptr(d_workspace), int(workspace_bytes),
                                 _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_compact") if check else rc

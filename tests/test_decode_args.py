@@ -286,3 +286,38 @@ def test_scales_of_other_types_and_shapes_are_refused(shape, dtype):
                dict(k_scale=Meta.of((2, 2))[:, 0], v_scale=scale)):
         with pytest.raises(ValueError):
             fdd.make_kv(pool, pool, **kw, **args)
+
+
+BAD_LISTS = [((3,), "int64"), ((3,), "float32"), ((2,), "int32"), ((0,), "int32"), ((3, 2), "int32")]  # the last: every second element
+
+
+@pytest.mark.parametrize("shape,dtype", BAD_LISTS)
+def test_lists_of_other_types_and_lengths_are_refused(shape, dtype):
+    """Three entries are asked for; nothing is launched."""
+    of, d, k = Meta.of, pages(), dict(stream=0, check=False)
+    bad = of(shape, dtype)[:, 0] if len(shape) == 2 else of(shape, dtype)
+    for args in ((bad, A, A, A), (A, bad, A, A), (A, A, A, bad)):
+        with pytest.raises(ValueError):
+            fdd.fdy_pages_extend(d, args[0], args[1], 3, args[2], args[3], 3, A, 1 << 50, A, **k)
+    for args in ((bad, A), (A, bad)):
+        with pytest.raises(ValueError):
+            fdd.fdy_pages_fork(d, *args, 3, A, 1 << 50, A, **k)
+        with pytest.raises(ValueError):
+            fdd.fdy_pages_copy(d, *args, 3, A, **k)
+    with pytest.raises(ValueError):
+        fdd.fdy_pages_free(d, bad, 3, A, **k)
+    with pytest.raises(ValueError):
+        fdd.fdy_pages_compact(pages(n_pages=3), bad, A, A, 1 << 50, A, **k)
+
+
+def test_other_arrays_of_calls_are_refused():
+    of, d, k = Meta.of, pages(), dict(stream=0, check=False)
+    for slots in (of(9, "int32"), of(8, "int64"), of((9, 2), "int64")[:, 0]):
+        with pytest.raises(ValueError):
+            fdd.fdy_pages_extend(d, A, A, 3, slots, A, 9, A, 1 << 50, A, **k)
+    for n_live in (of(1, "int64"), of(0, "int32")):
+        with pytest.raises(ValueError):
+            fdd.fdy_pages_compact(d, A, n_live, A, 1 << 50, A, **k)
+    for table in (of((4, 2, 32), "float64"), of((4, 2, 32), "bfloat16"), of((3, 2, 32)), of((4, 2, 64))[:, :, :32]):
+        with pytest.raises(ValueError):
+            fdd.fdy_rope_table(fdd.make_rope(64), 0, 4, table, **k)
