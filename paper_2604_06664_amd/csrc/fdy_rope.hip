@@ -44,14 +44,39 @@ struct Chunk {
   typedef float wide __attribute__((ext_vector_type(kN)));
 };
 
+// The scale of an 8-bit cache's head, by which elements are divided.  A product with the reciprocal is up to one and a half units
+// off; with its remainder, which a fused operation gives exactly, it becomes the quotient as rounded once (the reciprocal being
+// so itself, and nothing going out of range: elements are held within those that saturate, and other scales take the
+// division).  The bare product, this and the division throughout: 16,411 tokens of 40 heads 165, 165 and 176 us, 4,096 tokens of 8
+// cache heads 17.3, 18.0 and 19.9.
+struct Scale {
+  float by, inv, most;
+  bool tame;
+  __device__ explicit Scale(float s)
+      : by(s), inv(1.f / s), most(kF8Most * s), tame(s >= 0x1p-60f && s <= 0x1p60f) {}
+  __device__ __forceinline__ float quotient(float x) const {
+    const float y = __builtin_amdgcn_fmed3f(x, -most, most), q = y * inv;
+    return x != x ? x : __builtin_fmaf(-__builtin_fmaf(q, by, -y), inv, q);  // (this way round a zero keeps its sign)
+  }
+};
+
 // A chunk of elements to a cache: rounded once, to the cache's type.
 template <typename T, int kN, bool kF8>
-__device__ __forceinline__ void put(void* base, u64 at, typename Chunk<T, kN>::wide x, float inv) {
+__device__ __forceinline__ void put(void* base, u64 at, typename Chunk<T, kN>::wide x, const Scale& scale) {
   if (kF8) {
     typedef u32 words __attribute__((ext_vector_type(kN / 4)));
     words w;
+    if (scale.tame) {
 #pragma unroll
-    for (int i = 0; i < kN / 4; ++i) w[i] = to_f8x4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
+      for (int i = 0; i < kN; ++i) x[i] = scale.quotient(x[i]);
+#pragma unroll
+      for (int i = 0; i < kN / 4; ++i) w[i] = to_f8x4_in_range(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) x[i] /= scale.by;
+#pragma unroll
+      for (int i = 0; i < kN / 4; ++i) w[i] = to_f8x4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
     *(words*)((uint8_t*)base + at) = w;
   } else {
     typedef typename Chunk<T, kN>::raw raw;
@@ -84,7 +109,7 @@ struct Route {
   u64 to;
   void* cache;    // or null
   u64 in_cache;
-  float inv;      // 1 / scale of an 8-bit cache
+  float scale;    // of an 8-bit cache
   bool turned;
 };
 
@@ -94,7 +119,7 @@ __device__ __forceinline__ Route route_of(const Append& a, u32 t, u32 h, bool st
   const u32 nq = d.q ? d.n_q_heads : 0, nk = d.kv.n_heads;
   Route r;
   r.cache = nullptr;
-  r.inv = 1.f;
+  r.scale = 1.f;
   r.in_cache = 0;
   r.turned = h < nq + nk;
   if (h < nq) {
@@ -110,7 +135,7 @@ __device__ __forceinline__ Route route_of(const Append& a, u32 t, u32 h, bool st
     r.cache = key ? d.kv.k : d.kv.v;
     r.in_cache = page * d.kv.page_stride + place * d.kv.token_stride + g * d.kv.head_stride;
     const float* scale = key ? d.kv.k_scale : d.kv.v_scale;
-    if (kF8 && scale) r.inv = 1.f / scale[g];
+    if (kF8 && scale) r.scale = scale[g];
   }
   return r;
 }
@@ -180,12 +205,13 @@ __global__ void __launch_bounds__(256) append_kernel(Append a) {
       if (r[i].turned && turns) turn<wide, kN>(fa, fb, cs, sn, half);
       const u32 at = r[i].turned ? ta : va, bt = r[i].turned ? tb : vb;
       if (r[i].out) {
-        put<T, kN, false>(r[i].out, r[i].to + at, fa, 1.f);
-        if (bt < D) put<T, kN, false>(r[i].out, r[i].to + bt, fb, 1.f);
+        put<T, kN, false>(r[i].out, r[i].to + at, fa, Scale(1.f));
+        if (bt < D) put<T, kN, false>(r[i].out, r[i].to + bt, fb, Scale(1.f));
       }
       if (r[i].cache) {
-        put<T, kN, kF8>(r[i].cache, r[i].in_cache + at, fa, r[i].inv);
-        if (bt < D) put<T, kN, kF8>(r[i].cache, r[i].in_cache + bt, fb, r[i].inv);
+        const Scale scale(r[i].scale);
+        put<T, kN, kF8>(r[i].cache, r[i].in_cache + at, fa, scale);
+        if (bt < D) put<T, kN, kF8>(r[i].cache, r[i].in_cache + bt, fb, scale);
       }
     }
   }
@@ -198,7 +224,7 @@ __device__ __forceinline__ void put1(const Route& r, u32 e, float x) {
   if (r.out) ((elem*)r.out)[r.to + e] = (elem)x;
   if (r.cache) {
     if (kF8)
-      ((uint8_t*)r.cache)[r.in_cache + e] = (uint8_t)to_f8x4(x * r.inv, 0.f, 0.f, 0.f);
+      ((uint8_t*)r.cache)[r.in_cache + e] = (uint8_t)to_f8x4(x / r.scale, 0.f, 0.f, 0.f);
     else
       ((elem*)r.cache)[r.in_cache + e] = (elem)x;
   }

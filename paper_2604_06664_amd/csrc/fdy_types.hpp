@@ -26,10 +26,12 @@ __device__ __forceinline__ float f8_range(float x) {
   const float y = __builtin_amdgcn_fmed3f(x, -kF8Most, kF8Most);
   return x != x ? x : y;
 }
+__device__ __forceinline__ u32 to_f8x4_in_range(float a, float b, float c, float d) {
+  const int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (u32)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+}
 __device__ __forceinline__ u32 to_f8x4(float a, float b, float c, float d) {
-  int v = __builtin_amdgcn_cvt_pk_fp8_f32(f8_range(a), f8_range(b), 0, false);
-  v = __builtin_amdgcn_cvt_pk_fp8_f32(f8_range(c), f8_range(d), v, true);
-  return (u32)v;
+  return to_f8x4_in_range(f8_range(a), f8_range(b), f8_range(c), f8_range(d));
 }
 
 inline u32 log2_of(u32 v) { return 31u - (u32)__builtin_clz(v); }

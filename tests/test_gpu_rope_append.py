@@ -236,3 +236,48 @@ def test_cache_offsets_behind_32_bits(cache):
         y, size = od.turned(k[t].cpu().double(), table[int(pos[t])].cpu(), D, "half")
         close(got_k[t], y, size, cache)
         close(got_v[t], v[t].cpu().double(), v[t].cpu().double().abs(), cache)
+
+
+def quotients_next_to_ties():
+    """Scales, and elements for which x / scale and x * (1 / scale), in 32 bits, lie on two sides of a tie of e4m3 or on it."""
+    out = []
+    for m in range(1, 256):
+        for t in (17, 19, 21, 23, 25, 27, 29, 31):
+            s = np.float32(m) / np.float32(t)
+            for f in (np.nextafter(s, np.float32(0)), s, np.nextafter(s, np.float32(1e9))):
+                a, b = torch.tensor([m / f, np.float32(m) * (np.float32(1) / f)]).to(torch.float8_e4m3fn).float().tolist()
+                if a != b:
+                    out.append((m, float(f)))
+    return out
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("rot", [16, 8, 2])
+def test_eight_bit_elements_are_divided_by_their_scale(kind, rot):
+    """What is stored is the quotient in 32 bits, rounded: to the bit, as it is worked out on the CPU.  At position 0 keys are not
+    turned either.  Scales of the ends of the range, too."""
+    pairs = quotients_next_to_ties()
+    assert len(pairs) > 100
+    scales = sorted({f for _, f in pairs})[:200] + [2.0 ** -130, 2.0 ** -140, 2.0 ** -61, 2.0 ** 61, 1e30, -0.3, 1e-20]
+    H, D, T = len(scales), 64, 4
+    x = torch.randint(-255, 256, (T, H, D), generator=torch.Generator().manual_seed(3)).float()
+    x[..., :16] = torch.tensor([0.0, -0.0, 448.0, -448.0, 1e4, -1e4, 1e-6, 6e-5, float("inf"), float("-inf"), float("nan"), 1, 2, 3, 4, 5])
+    for h, s in enumerate(scales):
+        for j, (m, f) in enumerate([p for p in pairs if p[1] == s][:40]):
+            x[0, h, 20 + j] = m
+    x = x.to(DTYPES[kind])
+    f = torch.tensor(scales)
+    want = (x.float() / f[:, None]).clamp(-od.F8_MOST, od.F8_MOST).to(torch.float8_e4m3fn)
+    d_f, pools = f.to(DEV), [torch.zeros(1, 16, H, D, dtype=torch.uint8, device=DEV) for _ in "kv"]
+    kv = fdd.make_kv(*pools, type=fdd.FDY_F8, n_pages=1, page_tokens=16, n_heads=H, head_dim=D, page_stride=16 * H * D,
+                     token_stride=H * D, head_stride=D, k_scale=d_f, v_scale=d_f)
+    d = x.to(DEV)
+    table = table_of(rot, 1)
+    pos, slots = torch.zeros(T, dtype=torch.int32, device=DEV), torch.arange(T, device=DEV)
+    fdd.fdy_rope_append(fdd.make_append_desc(q=None, k=d, v=d, q_out=None, positions=pos, table=table, kv=kv, rot_dim=rot, slots=slots))
+    nan = torch.isnan(want.float())
+    for name, pool, first in (("v", pools[1], 0), ("k", pools[0], 16)):  # (an infinite key times a sine of 0 is no number)
+        got = pool[0, :T].cpu().view(torch.float8_e4m3fn)
+        assert torch.equal(torch.isnan(got.float())[..., first:], nan[..., first:]), name
+        a, b = (y.view(torch.uint8)[..., first:].clone() for y in (got, want))
+        assert torch.equal(a[~nan[..., first:]], b[~nan[..., first:]]), (name, int((a != b).sum()))
