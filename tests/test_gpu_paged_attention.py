@@ -499,3 +499,34 @@ def test_weights_are_held_in_more_bits_than_the_type_has(kind, cache, group):
     err = float(((out.double() - o).abs() / o).max())
     assert err <= ROUND[kind] + 2.0 ** -15 + 2.0 ** -16, err
     assert bool(((lse.double() - l).abs() <= 3e-5).all())
+
+
+def counters(p):
+    """Bytes of the workspace's counters: for each share and column, as many as there can be whatever the rows are (a column is 16 or
+    32 query heads of a cache head, a workgroup may take two or four of them).  Parts lie behind them."""
+    group = p.q.shape[1] // p.H
+    two = p.pt >= 16 and (p.D <= 128 or p.cache == "f8") and -(-group // 32) * 2 == -(-group // 16)
+    columns = p.H * -(-group // (32 if two else 16))
+    together = 4 if columns % 4 == 0 else 2 if columns % 2 == 0 else 1
+    return -(-max(columns, 512) * together * 4 // 256) * 256
+
+
+@pytest.mark.parametrize("Hq,H,D,cache", [(8, 2, 64, "bf16"), (16, 4, 128, "f8"), (5, 1, 256, "bf16"), (32, 1, 128, "bf16"), (100, 2, 64, "f8"),
+                                          (12, 12, 64, "bf16")])
+def test_all_counters_are_left_at_zero(Hq, H, D, cache):
+    """After every call over a shared workspace, whatever rows were in parts; parts were written where they are expected."""
+    rng = np.random.default_rng(51)
+    ragged = [int(x) for x in rng.integers(0, 700, 60)] + [2800, 1900]
+    problems = [Problem(lens, Hq, H, D, cache=cache, row_pages=pages) for lens in ([4000], [1, 700, 2300, 31], ragged, [9] * 40)
+                for pages in (256, WIDE)]
+    ws = torch.zeros(max(fdd.fdy_paged_attention_workspace_bytes(p.desc()) for p in problems), dtype=torch.uint8, device=DEV)
+    n = counters(problems[0])
+    for i in [0, 1, 2, 3, 4, 5, 6, 7, 4, 0, 6, 5, 1, 2]:
+        p = problems[i]
+        p.ws = ws
+        ws[n:] = 0
+        out, lse, _ = p.run()
+        assert p.ws is ws and bool((ws[:n] == 0).all()), i
+        if i < 2:
+            assert bool((ws[n:] != 0).any()), i
+        near((out, lse), p.want(), p.kind)
