@@ -20,7 +20,8 @@ using namespace fdy;
 
 namespace {
 
-constexpr u32 kTile = 32, kCus = 256;
+constexpr u32 kTile = 32;
+constexpr u32 kCus = 256;  // of the card: the workspace's size is asked for without a device
 constexpr u32 kEach = 3;  // what a row costs beside its tiles (queries, join, output), in tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 

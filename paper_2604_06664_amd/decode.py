@@ -129,8 +129,9 @@ def make_kv(k, v, *, type, n_pages, page_tokens, n_heads, head_dim, page_stride,
     """k, v: device pools (tensors or addresses) or None; strides in elements; scales float32 [n_heads]."""
     for name, x in (("k", k), ("v", v)):
         _pool(name, x, type, n_pages, page_tokens, n_heads, head_dim, page_stride, token_stride, head_stride)
-    _want("k_scale", k_scale, ["float32"], (n_heads,))
-    _want("v_scale", v_scale, ["float32"], (n_heads,))
+    if type == FDY_F8:  # others have none that is read
+        _want("k_scale", k_scale, ["float32"], (n_heads,))
+        _want("v_scale", v_scale, ["float32"], (n_heads,))
     return fdy_kv(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), page_stride, token_stride, head_stride, type, n_pages,
                   page_tokens, n_heads, head_dim, 0)
 
