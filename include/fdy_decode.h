@@ -12,7 +12,8 @@
  *     stays right while the sequences grow;
  *   - nothing is read back to the host, nothing is allocated, no memory is cleared by a memset.
  *
- * The conventions of fdy.h on memory, streams and errors hold (its integers do not: these work on floats): d_* / device pointers inside the descriptors are the caller's, descriptors are HOST
+ * The conventions of fdy.h on memory, streams and errors hold (its integers do not: these work on floats): d_* / device
+ * pointers inside the descriptors are the caller's, descriptors are HOST
  * structs that are read during the call only, calls only enqueue, return codes and status bits are those of fdy.h.  What
  * only the device can see (a length, a page number, a row number out of range) raises FDY_ST_BAD_INDEX and is skipped as
  * stated at each call.  Unless stated otherwise arrays that a call writes do not overlap arrays that it reads.
