@@ -5,7 +5,6 @@ taken from them; the caller keeps the tensors alive) and handed to every call.""
 from __future__ import annotations
 
 import ctypes as C
-import functools
 
 from . import FDY_ERR_INVALID_ARG, FDY_ERR_WORKSPACE, FDY_OK, FdyError, _check, _ptr, _stream, lib  # noqa: F401
 
@@ -86,17 +85,18 @@ def _want(name, x, types, shape):
         raise ValueError(f"{name}: {types[0]} {list(shape)}, contiguous, is wanted, not {x.dtype} {list(x.shape)}")
 
 
-@functools.lru_cache(maxsize=None)
-def _is(dtype, types):
-    return str(dtype) in [f"torch.{t}" for t in types]
+_names = {}  # of dtypes, as "int32"
 
 
 def _list(name, x, types, n):
-    """A tensor that a call reads or writes `n` elements of; made for every call, so short."""
-    if x is None or not hasattr(x, "is_contiguous"):
-        return
-    if not _is(x.dtype, types) or x.numel() < n or not x.is_contiguous():
-        raise ValueError(f"{name}: {types[0]}, contiguous, of {n} elements at least, is wanted, not {x.dtype} {list(x.shape)}")
+    """Address of a tensor that a call reads or writes `n` elements of.  Made for every call: a captured step's books are enqueued in
+    8 us, and each look at a tensor costs a tenth of one."""
+    if x is None or x.__class__ is int or not hasattr(x, "is_contiguous"):
+        return _ptr(x)
+    kind = x.dtype
+    if (_names.get(kind) or _names.setdefault(kind, str(kind).split(".")[-1])) not in types or x.numel() < n or not x.is_contiguous():
+        raise ValueError(f"{name}: {types[0]}, contiguous, of {n} elements at least, is wanted, not {kind} {list(x.shape)}")
+    return x.data_ptr()
 
 
 def _heads(name, x, like, shape):
@@ -197,8 +197,8 @@ def fdy_rope_frequencies(h_rope, check=True):
 
 
 def fdy_rope_table(h_rope, first, n_positions, d_table, stream=None, check=True):
-    _list("d_table", d_table, ("float32",), 0 if h_rope is None else int(n_positions) * h_rope.rot_dim)
-    rc = _L().fdy_rope_table(_d(h_rope), int(first), int(n_positions), _ptr(d_table), _stream(stream))
+    table = _list("d_table", d_table, ("float32",), 0 if h_rope is None else int(n_positions) * h_rope.rot_dim)
+    rc = _L().fdy_rope_table(_d(h_rope), int(first), int(n_positions), table, _stream(stream))
     return _check(rc, "fdy_rope_table") if check else rc
 
 
@@ -227,38 +227,33 @@ def fdy_pages_workspace_bytes(h_pages, n):
 
 def fdy_pages_extend(h_pages, d_rows, d_counts, n, d_slots, d_positions, n_slots, d_workspace, workspace_bytes,
                      d_status=None, stream=None, check=True):
-    for name, x, types, least in (("d_rows", d_rows, _I32, n), ("d_counts", d_counts, _I32, n), ("d_slots", d_slots, _I64, n_slots),
-                                  ("d_positions", d_positions, _I32, n_slots)):
-        _list(name, x, types, least)
-    rc = _L().fdy_pages_extend(_d(h_pages), _ptr(d_rows), _ptr(d_counts), int(n), _ptr(d_slots), _ptr(d_positions),
-                               int(n_slots), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    rows, counts = _list("d_rows", d_rows, _I32, n), _list("d_counts", d_counts, _I32, n)
+    slots, positions = _list("d_slots", d_slots, _I64, n_slots), _list("d_positions", d_positions, _I32, n_slots)
+    rc = _L().fdy_pages_extend(_d(h_pages), rows, counts, int(n), slots, positions, int(n_slots), _ptr(d_workspace),
+                               int(workspace_bytes), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_extend") if check else rc
 
 
 def fdy_pages_fork(h_pages, d_src, d_dst, n, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
-    _list("d_src", d_src, _I32, n)
-    _list("d_dst", d_dst, _I32, n)
-    rc = _L().fdy_pages_fork(_d(h_pages), _ptr(d_src), _ptr(d_dst), int(n), _ptr(d_workspace), int(workspace_bytes),
+    src, dst = _list("d_src", d_src, _I32, n), _list("d_dst", d_dst, _I32, n)
+    rc = _L().fdy_pages_fork(_d(h_pages), src, dst, int(n), _ptr(d_workspace), int(workspace_bytes),
                              _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_fork") if check else rc
 
 
 def fdy_pages_free(h_pages, d_rows, n, d_status=None, stream=None, check=True):
-    _list("d_rows", d_rows, _I32, n)
-    rc = _L().fdy_pages_free(_d(h_pages), _ptr(d_rows), int(n), _ptr(d_status), _stream(stream))
+    rc = _L().fdy_pages_free(_d(h_pages), _list("d_rows", d_rows, _I32, n), int(n), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_free") if check else rc
 
 
 def fdy_pages_copy(h_pages, d_src, d_dst, n, d_status=None, stream=None, check=True):
-    _list("d_src", d_src, _I32, n)
-    _list("d_dst", d_dst, _I32, n)
-    rc = _L().fdy_pages_copy(_d(h_pages), _ptr(d_src), _ptr(d_dst), int(n), _ptr(d_status), _stream(stream))
+    src, dst = _list("d_src", d_src, _I32, n), _list("d_dst", d_dst, _I32, n)
+    rc = _L().fdy_pages_copy(_d(h_pages), src, dst, int(n), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_copy") if check else rc
 
 
 def fdy_pages_compact(h_pages, d_map, d_n_live, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
-    _list("d_map", d_map, _I32, 0 if h_pages is None else h_pages.n_pages)
-    _list("d_n_live", d_n_live, _U32, 1)
-    rc = _L().fdy_pages_compact(_d(h_pages), _ptr(d_map), _ptr(d_n_live), _ptr(d_workspace), int(workspace_bytes),
-                                _ptr(d_status), _stream(stream))
+    to, n_live = _list("d_map", d_map, _I32, 0 if h_pages is None else h_pages.n_pages), _list("d_n_live", d_n_live, _U32, 1)
+    rc = _L().fdy_pages_compact(_d(h_pages), to, n_live, _ptr(d_workspace), int(workspace_bytes), _ptr(d_status),
+                                _stream(stream))
     return _check(rc, "fdy_pages_compact") if check else rc
