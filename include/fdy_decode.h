@@ -170,6 +170,108 @@ size_t fdy_paged_attention_workspace_bytes(const fdy_attend* h_desc);
 int fdy_paged_attention(const fdy_attend* h_desc, void* d_workspace, size_t workspace_bytes, uint32_t* d_status,
                         void* hip_stream);
 
+/* ---- attention of drafted tokens over the pages --------------------------------------------
+ * Several new tokens of every sequence at once, as a guess at what comes next that one pass verifies: the LAST c tokens of
+ * row r = rows[s] (s where rows is NULL) are drafted, c = first[s + 1] - first[s]; keys and values of all n = lens[r] lie in
+ * the pages already (fdy_pages_extend by c, fdy_rope_append with each token's position in the text), and drafted token i of
+ * the sequence is token n - c + i of the row and query first[s] + i of q.  With first NULL c is max_draft for every sequence.
+ *   query j sees the tokens t < n - c and, of the drafted ones, those whose bit i of sees[first[s] + j] is set (bit i % 64 of
+ *   word i / 64: the tokens that j goes on from, and itself; bits from c on are not looked at); sees NULL: those with i <= j,
+ *   which is a chain, or a piece of a prompt.
+ *   window w > 0: of what it sees only the last w tokens.
+ * Over these out, lse and their roundings are fdy_paged_attention's; a query that sees nothing: out 0, lse minus infinity.
+ * What a query does not see does not reach its result, infinities and NaN in another branch's keys and values included.
+ *   first not ascending, outside [0, n_tokens], or c > max_draft: the sequence is left out (its out and lse stay what they
+ *   were), FDY_ST_BAD_INDEX; queries that belong to no sequence stay what they were.  lens, rows and page numbers out of
+ *   range: as fdy_paged_attention; c > n: tokens ahead of the row's first are not there, FDY_ST_BAD_INDEX.  Sequences whose
+ *   queries overlap leave either's results there.
+ *   Alignment and strides: as fdy_paged_attention; sees 8-byte aligned, sees_words >= ceil(max_draft / 64) words a token,
+ *   at most 64 (0 with sees NULL); max_draft <= 1,024, n_tokens <= 2^23, n_tokens * n_q_heads <= 2^26, n_seqs <= 65,536; with first NULL
+ *   n_seqs * max_draft <= n_tokens; row_pages * page_tokens < 2^31; n_seqs * kv.n_heads * (ceil(max_draft * n_q_heads /
+ *   kv.n_heads / 16)) * (row_pages * page_tokens / 32 + 5) < 2^31.
+ *   workspace  as fdy_paged_attention's: cleared once, left cleared; one sized for a descriptor serves every one with the
+ *              same heads, head_dim, page_tokens and kv.type. */
+typedef struct {
+  const void* q;        /* [n_tokens][n_q_heads][head_dim] */
+  void* out;            /* [n_tokens][n_q_heads][head_dim] */
+  float* lse;           /* [n_tokens][n_q_heads] or NULL   */
+  const int32_t* table; /* [n_rows][row_pages]             */
+  const int32_t* lens;  /* [n_rows]                        */
+  const int32_t* rows;  /* [n_seqs] or NULL                */
+  const int32_t* first; /* [n_seqs + 1] or NULL            */
+  const uint64_t* sees; /* [n_tokens][sees_words] or NULL  */
+  uint64_t q_token, q_head, out_token, out_head; /* strides */
+  fdy_kv kv;
+  float scale;
+  uint32_t window; /* 0: none */
+  uint32_t n_seqs, n_q_heads, n_rows, row_pages, n_tokens, max_draft, sees_words;
+  uint32_t type; /* FDY_BF16 or FDY_F16 */
+} fdy_draft;     /* 216 B */
+size_t fdy_tree_attention_workspace_bytes(const fdy_draft* h_desc);
+int fdy_tree_attention(const fdy_draft* h_desc, void* d_workspace, size_t workspace_bytes, uint32_t* d_status,
+                       void* hip_stream);
+
+/* ---- attention over chosen pages -----------------------------------------------------------
+ * For contexts so long that reading all of them is what a step costs: a summary of every page's keys, kept as tokens come,
+ * tells which pages can matter to a query, and attention reads these.
+ *
+ * fdy_page_bounds: bounds[p][h][0][d] and [1][d] become the smallest and the largest element d of head h's keys among those
+ * tokens of page p that the row holds, in kv.type (of NaN and a number: NaN), for all pages in which one of the last
+ * min(fresh[s], lens[r]) tokens of row r = rows[s] lies (fresh NULL: 1 each); other pages' bounds stay.  Pages that rows of
+ * different lengths share get the bounds of either.  fresh[s] < 0 or > max_fresh: held within, FDY_ST_BAD_INDEX; rows, lens,
+ * page numbers out of range: as fdy_paged_attention.  kv.v is not read.
+ *   bounds and kv.k 16-byte aligned, kv's strides multiples of 16 bytes, head_dim of 16 bytes' elements; n_seqs <= 65,536,
+ *   row_pages * page_tokens < 2^31. */
+typedef struct {
+  void* bounds;         /* [kv.n_pages][kv.n_heads][2][head_dim], of kv.type */
+  const int32_t* table; /* [n_rows][row_pages] */
+  const int32_t* lens;  /* [n_rows]            */
+  const int32_t* rows;  /* [n_seqs] or NULL    */
+  const int32_t* fresh; /* [n_seqs] or NULL    */
+  fdy_kv kv;
+  uint32_t n_seqs, n_rows, row_pages, max_fresh;
+} fdy_bounds; /* 136 B */
+int fdy_page_bounds(const fdy_bounds* h_desc, uint32_t* d_status, void* hip_stream);
+
+/* fdy_page_select: of the P = ceil(n / page_tokens) pages of sequence s (row r = rows[s], n = lens[r]), for each cache head g,
+ * the `budget` that come first of: the row's first `sinks` and last `recent` pages; the others by
+ *   S_j = sum_d bounds[p_j][g][1][d] up_d + bounds[p_j][g][0][d] down_d,
+ *   up_d, down_d = the sums of the positive and of the negative elements d of k_scale[g] q_h over the query heads h of g,
+ * largest first, which no sum over h of a token's scores q_h . k in that page exceeds; ties go to the page nearer the row's
+ * beginning.  S is worked out in 64 bits.  A term whose up_d or down_d is 0 is 0; elements of q that are no number count in
+ * neither; an S that is no number counts as larger than all others.  Their page numbers go to pages[s][g][.] in the order of
+ * the row, -1 behind them; seen[s] = the number of tokens in them (the same for every head: all pages but the row's last are
+ * full), which with `pages` is what fdy_selected_attention takes.  P <= budget: all pages; n = 0: none.
+ *   rows, lens out of range: as fdy_paged_attention.  A page number outside [0, kv.n_pages) counts as S = minus infinity and
+ *   is passed on as it is where it is chosen, FDY_ST_BAD_INDEX.
+ *   q, bounds 16-byte aligned, q's strides multiples of 8 elements; kv gives type, n_pages, page_tokens, n_heads, head_dim and
+ *   k_scale (F8), its other fields are not read; recent >= 1, sinks + recent <= budget <= 2^25; n_seqs <= 65,536, n_q_heads a
+ *   multiple of kv.n_heads, n_seqs * n_q_heads <= 2^22, row_pages * page_tokens < 2^31, n_seqs * kv.n_heads * row_pages <= 2^32.
+ *   workspace  device, 256-byte aligned, fdy_page_select_workspace_bytes(), contents irrelevant; calls that share one must not
+ *              overlap in time. */
+typedef struct {
+  const void* q;        /* [n_seqs][n_q_heads][head_dim] */
+  const void* bounds;   /* fdy_page_bounds' */
+  const int32_t* table; /* [n_rows][row_pages] */
+  const int32_t* lens;  /* [n_rows]            */
+  const int32_t* rows;  /* [n_seqs] or NULL    */
+  int32_t* pages;       /* [n_seqs][kv.n_heads][budget] */
+  int32_t* seen;        /* [n_seqs]            */
+  uint64_t q_seq, q_head; /* strides */
+  fdy_kv kv;
+  uint32_t n_seqs, n_q_heads, n_rows, row_pages, budget, sinks, recent;
+  uint32_t type; /* FDY_BF16 or FDY_F16 */
+} fdy_select;    /* 184 B */
+size_t fdy_page_select_workspace_bytes(const fdy_select* h_desc);
+int fdy_page_select(const fdy_select* h_desc, void* d_workspace, size_t workspace_bytes, uint32_t* d_status, void* hip_stream);
+
+/* fdy_selected_attention: fdy_paged_attention with a list of pages for every cache head: table is
+ * [n_rows][kv.n_heads][row_pages] and token t of head g lies in page table[r][g][t / page_tokens]; lens, all else and the
+ * workspace (of the function below) as there.  n_rows * kv.n_heads < 2^31. */
+size_t fdy_selected_attention_workspace_bytes(const fdy_attend* h_desc);
+int fdy_selected_attention(const fdy_attend* h_desc, void* d_workspace, size_t workspace_bytes, uint32_t* d_status,
+                           void* hip_stream);
+
 /* ---- keeping the pages --------------------------------------------------------------------
  * A pool of n_pages pages that rows of pages share.  Its books are device arrays of the caller's:
  *   refs[p]       rows that hold page p (a row that holds it twice counts twice)
@@ -227,6 +329,27 @@ int fdy_pages_fork(const fdy_pages* h_pages, const int32_t* d_src, const int32_t
 
 /* Rows rows[i] give up their pages and become empty.  n <= 65,536 */
 int fdy_pages_free(const fdy_pages* h_pages, const int32_t* d_rows, uint32_t n, uint32_t* d_status, void* hip_stream);
+
+/* Of the last drafts[i] tokens of row rows[i] those with the numbers keep[i][0 .. kept[i]) among them (ascending, from 0) stay
+ * and move together: with b = lens[r] - drafts[i], token b + keep[i][j] becomes token b + j in all planes, lens[r] = b +
+ * kept[i], and pages that no longer hold a token of the row are given up (drafted tokens of which one path was accepted; a
+ * row that is held to its first and last tokens).  Positions that fdy_pages_extend gives count tokens, so after tokens are
+ * taken out of a text they are no longer the text's.
+ * In a page of a plane the bytes of token i are `pieces` pieces of piece_bytes, piece h at i * token_stride + h * piece_stride.
+ *   A row gets all or nothing.  It stays as it is, with FDY_ST_BAD_INDEX, where its number, its length, drafts[i] (below 0 or
+ *   above lens), kept[i] (below 0, above most or drafts[i]), keep[i] (not ascending, outside [0, drafts[i])) or a page number
+ *   that is needed is out of range, or the row was in the list before; and with FDY_ST_CAPACITY where a token would move into a
+ *   page that other rows hold too (refs > 1; what fdy_pages_extend has just given a row is its own).
+ *   piece_bytes, token_stride, piece_stride multiples of 16, pieces >= 1, a token's pieces lie within page_bytes (checked for
+ *   the last token of a page); pieces that overlap leave unspecified contents.  most <= 2^20, n <= 65,536, n * most < 2^31.
+ *   keep is [n][most].  Workspace: fdy_pages_workspace_bytes(h_pages, n). */
+typedef struct {
+  uint64_t token_stride, piece_stride; /* bytes */
+  uint32_t piece_bytes, pieces;
+} fdy_token; /* 24 B */
+int fdy_pages_keep(const fdy_pages* h_pages, const fdy_token* h_token, const int32_t* d_rows, const int32_t* d_drafts,
+                   const int32_t* d_keep, const int32_t* d_kept, uint32_t n, uint32_t most, void* d_workspace,
+                   size_t workspace_bytes, uint32_t* d_status, void* hip_stream);
 
 /* The contents of page src[i] to page dst[i] in all planes, i < n; no page may be both, or twice in dst.  The books stay
  * as they are. */

@@ -248,3 +248,142 @@ class Books:
             for j in range(self.pages_of(self.lens[r])):
                 self.table[r, j] = to[self.table[r, j]]
         return np.array(to, np.int32), n_live
+
+
+# ---- drafted tokens -----------------------------------------------------------------------------
+def tree_attend(q, k_view, v_view, table, lens, scale, drafts, sees=None, window=0, rows=None, k_scale=None, v_scale=None):
+    """q [tokens, heads, dim], drafts: drafted tokens of each sequence, one sequence after the other in q; sees: for each query
+    the numbers of the drafted tokens that it sees (None: those up to itself).  -> out, lse, spread as `attend`."""
+    T, Hq, D = q.shape
+    n_pages, pt, H, _ = k_view.shape
+    group = Hq // H
+    out, lse = torch.zeros(T, Hq, D, dtype=torch.float64), torch.full((T, Hq), -math.inf, dtype=torch.float64)
+    spread = torch.zeros(T, Hq, dtype=torch.float64)
+    query = 0
+    for s, c in enumerate(drafts):
+        r = s if rows is None else int(rows[s])
+        known = 0 <= r < table.shape[0]
+        n = min(max(int(lens[r]), 0), table.shape[1] * pt) if known else 0
+        for j in range(c):
+            own = range(j + 1) if sees is None else sorted(sees[query])
+            seen = list(range(n - c)) + [n - c + i for i in own if i < c]
+            if window:
+                seen = seen[max(0, len(seen) - window):]
+            at = [t for t in seen if 0 <= t < n and 0 <= int(table[r, t // pt]) < n_pages]
+            if at:
+                page, place = torch.tensor([int(table[r, t // pt]) for t in at]), torch.tensor([t % pt for t in at])
+                k, v = k_view[page, place].double(), v_view[page, place].double()
+                if k_scale is not None:
+                    k = k * k_scale.double()[:, None]
+                if v_scale is not None:
+                    v = v * v_scale.double()[:, None]
+                for h in range(Hq):
+                    x = scale * (k[:, h // group] @ q[query, h].double())
+                    m = x.max()
+                    if m == -math.inf:
+                        continue
+                    e = torch.exp(x - m)
+                    out[query, h] = (e[:, None] * v[:, h // group]).sum(0) / e.sum()
+                    lse[query, h] = m + torch.log(e.sum())
+                    spread[query, h] = v[:, h // group].abs().max()
+            query += 1
+    return out, lse, spread
+
+
+# ---- chosen pages -------------------------------------------------------------------------------
+def page_bounds(bounds, k_view, table, lens, fresh, max_fresh=1 << 31, rows=None):
+    """Writes bounds [page, head, 2, dim] (64 bits) of the pages that hold one of each row's last `fresh` tokens."""
+    pt = k_view.shape[1]
+    for s, f in enumerate(fresh):
+        r = s if rows is None else int(rows[s])
+        if not 0 <= r < table.shape[0]:
+            continue
+        n = min(max(int(lens[r]), 0), table.shape[1] * pt)
+        f = min(max(int(f), 0), max_fresh, n)
+        for j in range(table.shape[1]):
+            held = [t for t in range(j * pt, min(n, (j + 1) * pt))]
+            p = int(table[r, j])
+            if held and held[-1] >= n - f and 0 <= p < len(bounds):
+                k = k_view[p, :len(held)].double()
+                bounds[p, :, 0], bounds[p, :, 1] = k.amin(0), k.amax(0)
+
+
+def page_scores(q, bounds, pages, n_pages, k_scale=None):
+    """S of the pages of one sequence, [head][page]: q [heads, dim], bounds [page, head, 2, dim]; sums rounded once."""
+    H, D = bounds.shape[1], bounds.shape[3]
+    q = q.double().view(H, -1, D)
+    if k_scale is not None:
+        q = q * k_scale.double()[:, None, None]
+    out = []
+    for g in range(H):
+        up = [math.fsum(x for x in q[g, :, d].tolist() if x > 0) for d in range(D)]
+        down = [math.fsum(x for x in q[g, :, d].tolist() if x < 0) for d in range(D)]
+        row = []
+        for p in pages:
+            p = int(p)
+            if not 0 <= p < n_pages:
+                row.append(-math.inf)
+                continue
+            low, high = bounds[p, g, 0].tolist(), bounds[p, g, 1].tolist()
+            terms = [h * u for h, u in zip(high, up) if u != 0] + [b * d for b, d in zip(low, down) if d != 0]
+            inf = {t for t in terms if math.isinf(t)}
+            if any(math.isnan(t) for t in terms) or len(inf) == 2:
+                row.append(math.nan)
+            else:
+                row.append(inf.pop() if inf else math.fsum(terms))
+        out.append(row)
+    return out
+
+
+def page_select(q, bounds, table, lens, page_tokens, budget, sinks, recent, rows=None, k_scale=None):
+    """-> pages [seq, head, budget], seen [seq]."""
+    B, H, n_pages = q.shape[0], bounds.shape[1], bounds.shape[0]
+    pages, seen = np.full((B, H, budget), -1, np.int32), np.zeros(B, np.int32)
+    for s in range(B):
+        r = s if rows is None else int(rows[s])
+        if not 0 <= r < table.shape[0]:
+            continue
+        n = min(max(int(lens[r]), 0), table.shape[1] * page_tokens)
+        P = -(-n // page_tokens)
+        taken = min(P, budget)
+        seen[s] = n - (P - taken) * page_tokens
+        scores = page_scores(q[s], bounds, table[r, :P], n_pages, k_scale) if P > budget else [[0.0] * P] * H
+        for g in range(H):
+            first = lambda j: j < sinks or j >= P - recent  # noqa: E731
+            rank = lambda x: (1, 0.0) if math.isnan(x) else (0, x)  # noqa: E731
+            order = sorted(range(P), key=lambda j: (not first(j), tuple(-y for y in rank(scores[g][j])) if not first(j) else (0, 0), j))
+            pages[s, g, :taken] = [table[r, j] for j in sorted(order[:taken])]
+    return pages, seen
+
+
+def keep(books, rows, drafts, keep_lists):
+    """fdy_pages_keep on `Books` whose planes are [plane, page, token, ...]; keep_lists: numbers that stay, for each row."""
+    refs, served, seen = list(books.refs), [], set()
+    for i, r in enumerate(rows):
+        r, c, ks = int(r), int(drafts[i]), [int(k) for k in keep_lists[i]]
+        ok = 0 <= r < len(books.lens) and r not in seen
+        seen.add(r)
+        n = books.lens[r] if ok else 0
+        ok = ok and 0 <= n <= books.table.shape[1] * books.pt and 0 <= c <= n and len(ks) <= c
+        ok = ok and all(0 <= k < c for k in ks) and all(a < b for a, b in zip(ks, ks[1:]))
+        if ok:
+            base = n - c
+            moves = [(base + k, base + j) for j, k in enumerate(ks) if k != j]
+            page = lambda t: int(books.table[r, t // books.pt])  # noqa: E731
+            gone = [int(p) for p in books.table[r, books.pages_of(base + len(ks)):books.pages_of(n)]]
+            needed = [page(t) for m in moves for t in m] + gone
+            ok = all(0 <= p < len(refs) for p in needed)
+        if not ok:
+            books.status |= ST_BAD_INDEX
+        elif any(refs[page(b)] > 1 for _, b in moves):
+            books.status |= ST_CAPACITY
+        else:
+            served.append((r, base, len(ks), [(page(a), a % books.pt, page(b), b % books.pt) for a, b in moves], gone))
+    for r, base, kept, moves, gone in served:
+        if books.planes is not None and moves:
+            before = books.planes.copy()
+            for p, i, q, j in moves:
+                books.planes[:, q, j] = before[:, p, i]
+        for p in gone:
+            books.refs[p] -= 1
+        books.lens[r] = base + kept

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libfdy.so")
 SOURCES = ["fdy_api.hip", "fdy_scan.hip", "fdy_fingerprint.hip", "fdy_materialize.hip", "fdy_derive.hip",
            "fdy_arena.hip", "fdy_archive.hip", "fdy_rope.hip", "fdy_attention.hip",
-           "fdy_pages.hip"]
+           "fdy_pages.hip", "fdy_select.hip", "fdy_tree.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra",
     "-Wno-unused-parameter",

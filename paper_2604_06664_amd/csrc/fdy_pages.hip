@@ -39,12 +39,14 @@ __device__ __forceinline__ u32 length_of(const Pages& a, u32 row, bool& bad) {
   return n < 0 ? 0 : most;
 }
 
-__device__ __forceinline__ void set_free(const Pages& a, u32 page) {
+template <typename A>
+__device__ __forceinline__ void set_free(const A& a, u32 page) {
   atomicOr((u32*)a.d.free_bits + (page >> 5), 1u << (page & 31));
 }
 
 // One holder less; nobody left: the page is free.  False: nobody held it.
-__device__ __forceinline__ bool drop(const Pages& a, u32 page) {
+template <typename A>
+__device__ __forceinline__ bool drop(const A& a, u32 page) {
   const u32 before = atomicSub(a.d.refs + page, 1u);
   if (before == 1) set_free(a, page);
   if (before == 0) atomicAdd(a.d.refs + page, 1u);
@@ -477,6 +479,96 @@ __global__ void __launch_bounds__(256) free_kernel(Pages a) {
   if (bad) raise_status(a.status, FDY_ST_BAD_INDEX);
 }
 
+// ---- keep -------------------------------------------------------------------------------------------
+// First all rows are looked at (a row is served or not by what was there before the call), then tokens move and books change.
+// Words of the workspace, an entry: first token that moves (kUnserved: the row stays as it is), tokens ahead of the drafted
+// ones, tokens that stay, and the row's length.
+struct KeepArg {
+  fdy_pages d;
+  fdy_token t;
+  u32* status;
+  const int32_t *rows, *drafts, *keep, *kept;
+  u32* ws;
+  u32 n, most, shift, columns;  // columns: 16-byte words of a token in a plane
+};
+typedef Arg<KeepArg> Keep;
+
+__global__ void __launch_bounds__(256) keep_plan_kernel(Keep a) {
+  __shared__ u32 s_moves;
+  const u32 i = blockIdx.x, r = (u32)a.rows[i], tid = threadIdx.x;
+  const int drafts = a.drafts[i], kept = a.kept[i];
+  u32* plan = a.ws + 4 * i;
+  u32 wrong = 0;
+  if (tid == 0) s_moves = kept > 0 ? (u32)kept : 0;
+  __syncthreads();
+  bool bad = r >= a.d.n_rows || named_before(a.rows, i);
+  u32 n = 0;
+  if (!bad) n = (u32)a.d.lens[r], bad = n > a.d.row_pages << a.shift;
+  bad = bad || drafts < 0 || (u32)drafts > n || kept < 0 || kept > drafts || (u32)kept > a.most;
+  if (!bad) {
+    const u32 base = n - (u32)drafts;
+    const int32_t *keep = a.keep + (u64)i * a.most, *table = a.d.table + (u64)r * a.d.row_pages;
+    for (u32 j = tid; j < (u32)kept; j += 256) {
+      const int k = keep[j], before = j ? keep[j - 1] : -1;
+      if (k <= before || k >= drafts) {
+        wrong |= FDY_ST_BAD_INDEX;
+      } else if ((u32)k != j) {  // it moves (from the first such on all do)
+        atomicMin(&s_moves, j);
+        const u32 from = (u32)table[(base + (u32)k) >> a.shift], to = (u32)table[(base + j) >> a.shift];
+        if (from >= a.d.n_pages || to >= a.d.n_pages)
+          wrong |= FDY_ST_BAD_INDEX;
+        else if (a.d.refs[to] > 1)
+          wrong |= FDY_ST_CAPACITY;
+      }
+    }
+    const u32 in_page = a.d.page_tokens - 1;
+    for (u32 j = ((base + (u32)kept + in_page) >> a.shift) + tid; j < (n + in_page) >> a.shift; j += 256)  // those given up
+      if ((u32)table[j] >= a.d.n_pages) wrong |= FDY_ST_BAD_INDEX;
+  }
+  if (bad) wrong = FDY_ST_BAD_INDEX;
+  const bool refused = __syncthreads_or((int)(wrong & FDY_ST_BAD_INDEX)), shared = __syncthreads_or((int)(wrong & FDY_ST_CAPACITY));
+  if (tid) return;
+  if (refused || shared) raise_status(a.status, refused ? FDY_ST_BAD_INDEX : FDY_ST_CAPACITY);
+  plan[0] = refused || shared ? kUnserved : s_moves;
+  plan[1] = n - (u32)drafts, plan[2] = (u32)kept, plan[3] = n;
+}
+
+// A lane takes one 16-byte word of the row's tokens in one plane and moves it for one token after the other, so that a place is
+// read before it is written to: tokens only move to the front.  Eight of them are under way together.
+constexpr u32 kMoved = 8;
+__global__ void __launch_bounds__(256) keep_move_kernel(Keep a) {
+  const u32 i = blockIdx.x;
+  const u32* plan = a.ws + 4 * i;
+  const u32 begin = uniform(plan[0]), base = uniform(plan[1]), kept = uniform(plan[2]), n = uniform(plan[3]);
+  if (begin == kUnserved) return;
+  const u32 r = (u32)a.rows[i], in_page = a.d.page_tokens - 1;
+  const int32_t *table = a.d.table + (u64)r * a.d.row_pages, *keep = a.keep + (u64)i * a.most;
+  const u32 words = a.t.piece_bytes / 16;
+  const u64 all = (u64)a.columns * a.d.n_planes;
+  for (u64 c = blockIdx.y * 256 + threadIdx.x; begin < kept && c < all; c += gridDim.y * 256) {
+    const u32 plane = (u32)(c / a.columns), at = (u32)(c - (u64)plane * a.columns), piece = at / words;
+    uint8_t* const of = (uint8_t*)a.d.planes[plane] + piece * a.t.piece_stride + (at - piece * words) * 16;
+    auto place = [&](u32 token) {
+      return (v4u32*)(of + (u32)table[token >> a.shift] * a.d.page_stride + (token & in_page) * a.t.token_stride);
+    };
+    for (u32 j0 = begin; j0 < kept; j0 += kMoved) {
+      v4u32 x[kMoved];
+#pragma unroll
+      for (u32 j = 0; j < kMoved; ++j)
+        if (j0 + j < kept) x[j] = *place(base + (u32)keep[j0 + j]);
+#pragma unroll
+      for (u32 j = 0; j < kMoved; ++j)
+        if (j0 + j < kept) *place(base + j0 + j) = x[j];
+    }
+  }
+  if (blockIdx.y) return;
+  bool bad = false;
+  for (u32 j = ((base + kept + in_page) >> a.shift) + threadIdx.x; j < (n + in_page) >> a.shift; j += 256)
+    if (!drop(a, (u32)table[j])) bad = true;
+  if (threadIdx.x == 0) a.d.lens[r] = (int32_t)(base + kept);
+  if (bad) raise_status(a.status, FDY_ST_BAD_INDEX);
+}
+
 // ---- copy -------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(256) copy_kernel(Pages a) {
   const u32 i = blockIdx.x, s = (u32)a.from[i], d = (u32)a.to[i];
@@ -618,8 +710,8 @@ Pages args(const fdy_pages* h, u32 n, void* ws, u32* status) {
   return a;
 }
 
-template <typename K>
-int go(K kernel, dim3 grid, u32 threads, void* stream, const Pages& a) {
+template <typename K, typename A>
+int go(K kernel, dim3 grid, u32 threads, void* stream, const A& a) {
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, (hipStream_t)stream, a);
   FDY_HIP_TRY(hipGetLastError());
@@ -689,6 +781,39 @@ extern "C" int fdy_pages_free(const fdy_pages* h, const int32_t* d_rows, uint32_
   Pages a = args(h, n, nullptr, d_status);
   a.from = d_rows;
   return go(free_kernel, dim3(n), 256, stream, a);
+}
+
+extern "C" int fdy_pages_keep(const fdy_pages* h, const fdy_token* h_token, const int32_t* d_rows, const int32_t* d_drafts,
+                              const int32_t* d_keep, const int32_t* d_kept, uint32_t n, uint32_t most, void* ws, size_t ws_bytes,
+                              uint32_t* d_status, void* stream) {
+  int rc = check(h, true, true);
+  if (rc != FDY_OK) return rc;
+  if (!h_token || n > kMostEntries || most > 1u << 20 || (u64)n * most >> 31) return FDY_ERR_INVALID_ARG;
+  const fdy_token& t = *h_token;
+  if (h->n_planes) {
+    if (!t.pieces || !t.piece_bytes || (t.token_stride | t.piece_stride | t.piece_bytes) % 16) return FDY_ERR_INVALID_ARG;
+    if (t.token_stride >> 30 || t.piece_stride >> 30 ||
+        (h->page_tokens - 1) * t.token_stride + (t.pieces - 1) * t.piece_stride + t.piece_bytes > h->page_bytes ||
+        (u64)t.pieces * t.piece_bytes > h->page_bytes)
+      return FDY_ERR_INVALID_ARG;
+  }
+  if (!aligned(d_rows, 4) || !aligned(d_drafts, 4) || !aligned(d_keep, 4) || !aligned(d_kept, 4)) return FDY_ERR_INVALID_ARG;
+  if (n == 0) return FDY_OK;
+  if (!d_rows || !d_drafts || !d_kept || (!d_keep && most)) return FDY_ERR_INVALID_ARG;
+  if (workspace_bad(h, n, ws, ws_bytes)) return FDY_ERR_WORKSPACE;
+  Keep a{};
+  a.d = *h;
+  a.t = t;
+  a.status = d_status;
+  a.rows = d_rows, a.drafts = d_drafts, a.keep = d_keep, a.kept = d_kept;
+  a.ws = (u32*)ws;
+  a.n = n, a.most = most;
+  a.shift = log2_of(h->page_tokens);
+  a.columns = h->n_planes ? t.pieces * (t.piece_bytes / 16) : 0;
+  rc = go(keep_plan_kernel, dim3(n), 256, stream, a);
+  if (rc != FDY_OK) return rc;
+  const u64 blocks = ((u64)a.columns * h->n_planes + 255) / 256;
+  return go(keep_move_kernel, dim3(n, at_most(blocks + (blocks == 0), 1024)), 256, stream, a);
 }
 
 extern "C" int fdy_pages_copy(const fdy_pages* h, const int32_t* d_src, const int32_t* d_dst, uint32_t n,

@@ -31,6 +31,14 @@ fdy_append = _struct("fdy_append", ("q", "k", "v", "q_out", "k_out", "positions"
 fdy_attend = _struct("fdy_attend", ("q", "out", "lse", "table", "lens", "rows"), ("q_seq", "q_head", "out_seq", "out_head"),
                      [("kv", fdy_kv), ("scale", C.c_float)],
                      ("window", "n_seqs", "n_q_heads", "n_rows", "row_pages", "type", "reserved"))
+fdy_draft = _struct("fdy_draft", ("q", "out", "lse", "table", "lens", "rows", "first", "sees"),
+                    ("q_token", "q_head", "out_token", "out_head"), [("kv", fdy_kv), ("scale", C.c_float)],
+                    ("window", "n_seqs", "n_q_heads", "n_rows", "row_pages", "n_tokens", "max_draft", "sees_words", "type"))
+fdy_bounds = _struct("fdy_bounds", ("bounds", "table", "lens", "rows", "fresh"), (), [("kv", fdy_kv)],
+                     ("n_seqs", "n_rows", "row_pages", "max_fresh"))
+fdy_select = _struct("fdy_select", ("q", "bounds", "table", "lens", "rows", "pages", "seen"), ("q_seq", "q_head"), [("kv", fdy_kv)],
+                     ("n_seqs", "n_q_heads", "n_rows", "row_pages", "budget", "sinks", "recent", "type"))
+fdy_token = _struct("fdy_token", (), ("token_stride", "piece_stride"), (), ("piece_bytes", "pieces"))
 fdy_pages = _struct("fdy_pages", ("refs", "free_bits", "table", "lens", "planes"), ("page_bytes", "page_stride"), (),
                     ("n_pages", "page_tokens", "n_rows", "row_pages", "n_planes", "reserved"))
 
@@ -54,6 +62,14 @@ def _L():
                 ("fdy_rope_append", i, [p, p, p]),
                 ("fdy_paged_attention_workspace_bytes", z, [p]),
                 ("fdy_paged_attention", i, [p, p, z, p, p]),
+                ("fdy_tree_attention_workspace_bytes", z, [p]),
+                ("fdy_tree_attention", i, [p, p, z, p, p]),
+                ("fdy_page_bounds", i, [p, p, p]),
+                ("fdy_page_select_workspace_bytes", z, [p]),
+                ("fdy_page_select", i, [p, p, z, p, p]),
+                ("fdy_selected_attention_workspace_bytes", z, [p]),
+                ("fdy_selected_attention", i, [p, p, z, p, p]),
+                ("fdy_pages_keep", i, [p, p, p, p, p, p, u, u, p, z, p, p]),
                 ("fdy_pages_reset", i, [p, p]),
                 ("fdy_pages_workspace_bytes", z, [p, u]),
                 ("fdy_pages_extend", i, [p, p, p, u, p, p, u, p, z, p, p]),
@@ -170,6 +186,68 @@ def make_attend_desc(*, q, out, table, lens, kv, scale, lse=None, rows=None, win
     return d
 
 
+def make_draft_desc(*, q, out, table, lens, kv, scale, max_draft, first=None, sees=None, lse=None, rows=None, window=0):
+    """q, out: tensors [tokens, heads, dim] with contiguous last dimension, the sequences' drafted tokens one after the other;
+    first [sequences + 1] 32-bit (None: max_draft tokens each); sees [tokens, words] of 64 bits (None: chains)."""
+    for name, x in (("q", q), ("out", out)):
+        _heads(name, x, q, (q.shape[0], q.shape[1], kv.head_dim))
+    n_seqs = first.shape[0] - 1 if first is not None else q.shape[0] // max(1, max_draft)
+    _want("table", table, ["int32"], table.shape[:2])
+    _want("lens", lens, ["int32"], table.shape[:1])
+    _want("rows", rows, ["int32"], (n_seqs,))
+    _want("first", first, ["int32"], (n_seqs + 1,))
+    _want("sees", sees, ["int64", "uint64"], q.shape[:1] + (0 if sees is None else sees.shape[1],))
+    _want("lse", lse, ["float32"], q.shape[:2])
+    return fdy_draft(_ptr(q), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), _ptr(rows), _ptr(first), _ptr(sees), q.stride(0),
+                     q.stride(1), out.stride(0), out.stride(1), kv, scale, window, n_seqs, q.shape[1], table.shape[0],
+                     table.shape[1], q.shape[0], max_draft, 0 if sees is None else sees.shape[1], type_of(q))
+
+
+def make_bounds_desc(*, bounds, table, lens, kv, fresh=None, rows=None, max_fresh=1):
+    """bounds [pages, heads, 2, dim] of the cache's type; one sequence for each of rows, or for each row of the table."""
+    n_seqs = (table if rows is None else rows).shape[0]
+    _want("bounds", bounds, [_KV_TYPES[kv.type].split(".")[1], "uint8" if kv.type == FDY_F8 else "int16"],
+          (kv.n_pages, kv.n_heads, 2, kv.head_dim))
+    _want("table", table, ["int32"], table.shape[:2])
+    _want("lens", lens, ["int32"], table.shape[:1])
+    _want("rows", rows, ["int32"], (n_seqs,))
+    _want("fresh", fresh, ["int32"], (n_seqs,))
+    return fdy_bounds(_ptr(bounds), _ptr(table), _ptr(lens), _ptr(rows), _ptr(fresh), kv, n_seqs, table.shape[0], table.shape[1],
+                      max_fresh)
+
+
+def make_select_desc(*, q, bounds, table, lens, kv, pages, seen, sinks=1, recent=1, rows=None):
+    """q [sequences, heads, dim] with contiguous last dimension; pages [sequences, cache heads, budget] and seen receive the choice.
+    kv: of make_kv; its pools may be None here."""
+    _heads("q", q, q, (q.shape[0], q.shape[1], kv.head_dim))
+    _want("bounds", bounds, [_KV_TYPES[kv.type].split(".")[1], "uint8" if kv.type == FDY_F8 else "int16"],
+          (kv.n_pages, kv.n_heads, 2, kv.head_dim))
+    _want("table", table, ["int32"], table.shape[:2])
+    _want("lens", lens, ["int32"], table.shape[:1])
+    _want("rows", rows, ["int32"], q.shape[:1])
+    _want("pages", pages, ["int32"], (q.shape[0], kv.n_heads, pages.shape[2]))
+    _want("seen", seen, ["int32"], q.shape[:1])
+    return fdy_select(_ptr(q), _ptr(bounds), _ptr(table), _ptr(lens), _ptr(rows), _ptr(pages), _ptr(seen), q.stride(0), q.stride(1),
+                      kv, q.shape[0], q.shape[1], table.shape[0], table.shape[1], pages.shape[2], sinks, recent, type_of(q))
+
+
+def make_selected_desc(*, q, out, table, lens, kv, scale, lse=None, rows=None, window=0):
+    """As make_attend_desc, with table [rows, cache heads, pages]: a list of pages for every cache head."""
+    for name, x in (("q", q), ("out", out)):
+        _heads(name, x, q, (q.shape[0], q.shape[1], kv.head_dim))
+    _want("table", table, ["int32"], (table.shape[0], kv.n_heads, table.shape[2]))
+    _want("lens", lens, ["int32"], table.shape[:1])
+    _want("rows", rows, ["int32"], q.shape[:1])
+    _want("lse", lse, ["float32"], q.shape[:2])
+    return fdy_attend(_ptr(q), _ptr(out), _ptr(lse), _ptr(table), _ptr(lens), _ptr(rows), q.stride(0), q.stride(1), out.stride(0),
+                      out.stride(1), kv, scale, window, q.shape[0], q.shape[1], table.shape[0], table.shape[2], type_of(q), 0)
+
+
+def make_token(*, token_stride, piece_bytes, pieces=1, piece_stride=0):
+    """Where a token's bytes lie in a page of a plane; strides and sizes in bytes."""
+    return fdy_token(token_stride, piece_stride, piece_bytes, pieces)
+
+
 def make_pages(*, refs, free_bits, table, lens, page_tokens, planes=None, page_bytes=0, page_stride=0):
     """refs [pages], table [rows, pages of a row], lens [rows], 32-bit; free_bits, planes (device addresses) 64-bit."""
     _want("refs", refs, ["int32", "uint32"], refs.shape[:1])
@@ -216,6 +294,38 @@ def fdy_paged_attention(h_desc, d_workspace, workspace_bytes, d_status=None, str
     return _check(rc, "fdy_paged_attention") if check else rc
 
 
+def fdy_tree_attention_workspace_bytes(h_desc):
+    return _L().fdy_tree_attention_workspace_bytes(_d(h_desc))
+
+
+def fdy_tree_attention(h_desc, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    rc = _L().fdy_tree_attention(_d(h_desc), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_tree_attention") if check else rc
+
+
+def fdy_page_bounds(h_desc, d_status=None, stream=None, check=True):
+    rc = _L().fdy_page_bounds(_d(h_desc), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_page_bounds") if check else rc
+
+
+def fdy_page_select_workspace_bytes(h_desc):
+    return _L().fdy_page_select_workspace_bytes(_d(h_desc))
+
+
+def fdy_page_select(h_desc, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    rc = _L().fdy_page_select(_d(h_desc), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_page_select") if check else rc
+
+
+def fdy_selected_attention_workspace_bytes(h_desc):
+    return _L().fdy_selected_attention_workspace_bytes(_d(h_desc))
+
+
+def fdy_selected_attention(h_desc, d_workspace, workspace_bytes, d_status=None, stream=None, check=True):
+    rc = _L().fdy_selected_attention(_d(h_desc), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_selected_attention") if check else rc
+
+
 def fdy_pages_reset(h_pages, stream=None, check=True):
     rc = _L().fdy_pages_reset(_d(h_pages), _stream(stream))
     return _check(rc, "fdy_pages_reset") if check else rc
@@ -244,6 +354,14 @@ def fdy_pages_fork(h_pages, d_src, d_dst, n, d_workspace, workspace_bytes, d_sta
 def fdy_pages_free(h_pages, d_rows, n, d_status=None, stream=None, check=True):
     rc = _L().fdy_pages_free(_d(h_pages), _list("d_rows", d_rows, _I32, n), int(n), _ptr(d_status), _stream(stream))
     return _check(rc, "fdy_pages_free") if check else rc
+
+
+def fdy_pages_keep(h_pages, h_token, d_rows, d_drafts, d_keep, d_kept, n, most, d_workspace, workspace_bytes, d_status=None,
+                   stream=None, check=True):
+    rows, drafts, kept = _list("d_rows", d_rows, _I32, n), _list("d_drafts", d_drafts, _I32, n), _list("d_kept", d_kept, _I32, n)
+    rc = _L().fdy_pages_keep(_d(h_pages), _d(h_token), rows, drafts, _list("d_keep", d_keep, _I32, int(n) * int(most)), kept, int(n),
+                             int(most), _ptr(d_workspace), int(workspace_bytes), _ptr(d_status), _stream(stream))
+    return _check(rc, "fdy_pages_keep") if check else rc
 
 
 def fdy_pages_copy(h_pages, d_src, d_dst, n, d_status=None, stream=None, check=True):
