@@ -132,16 +132,6 @@ __device__ __forceinline__ Span span_of(const A& a, u32 s) {
   return r;
 }
 
-template <typename T>
-__device__ __forceinline__ T wave_incl_most(T v) {
-  v = max(v, dpp<kShr1>(v, (T)0));
-  v = max(v, dpp<kShr2>(v, (T)0));
-  v = max(v, dpp<kShr4>(v, (T)0));
-  v = max(v, dpp<kShr8>(v, (T)0));
-  v = max(v, dpp<kOfRow, 0xa>(v, (T)0));
-  return max(v, dpp<kOfHalf, 0xc>(v, (T)0));
-}
-
 // ---- loads ------------------------------------------------------------------------------------------
 // Keys and values that are read once are marked so (two rows of 10^5 tokens: 171 us, marked 154); those of query heads that
 // take several workgroups are read by each, and not.

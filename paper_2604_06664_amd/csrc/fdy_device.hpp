@@ -117,6 +117,17 @@ __device__ __forceinline__ T wave_incl_scan(T v) {
   return v;
 }
 
+// The same with the largest in place of the sum.
+template <typename T>
+__device__ __forceinline__ T wave_incl_most(T v) {
+  v = max(v, dpp<kShr1>(v, (T)0));
+  v = max(v, dpp<kShr2>(v, (T)0));
+  v = max(v, dpp<kShr4>(v, (T)0));
+  v = max(v, dpp<kShr8>(v, (T)0));
+  v = max(v, dpp<kOfRow, 0xa>(v, (T)0));
+  return max(v, dpp<kOfHalf, 0xc>(v, (T)0));
+}
+
 // Exclusive scan of one u64 per thread over a workgroup of whole waves (at most 1024 threads);
 // returns the exclusive prefix and sets `total` (same in every thread).  s_buf: 17 u64 of LDS.
 __device__ inline u64 block_excl_scan(u64 v, u64* s_buf, u64& total) {

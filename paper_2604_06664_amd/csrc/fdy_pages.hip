@@ -493,7 +493,7 @@ struct KeepArg {
 };
 typedef Arg<KeepArg> Keep;
 
-__global__ void __launch_bounds__(256) keep_plan_kernel(Keep a) {
+__global__ void __launch_bounds__(1024) keep_plan_kernel(Keep a) {
   __shared__ u32 s_moves;
   const u32 i = blockIdx.x, r = (u32)a.rows[i], tid = threadIdx.x;
   const int drafts = a.drafts[i], kept = a.kept[i];
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(256) keep_plan_kernel(Keep a) {
   if (!bad) {
     const u32 base = n - (u32)drafts;
     const int32_t *keep = a.keep + (u64)i * a.most, *table = a.d.table + (u64)r * a.d.row_pages;
-    for (u32 j = tid; j < (u32)kept; j += 256) {
+    for (u32 j = tid; j < (u32)kept; j += blockDim.x) {
       const int k = keep[j], before = j ? keep[j - 1] : -1;
       if (k <= before || k >= drafts) {
         wrong |= FDY_ST_BAD_INDEX;
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(256) keep_plan_kernel(Keep a) {
       }
     }
     const u32 in_page = a.d.page_tokens - 1;
-    for (u32 j = ((base + (u32)kept + in_page) >> a.shift) + tid; j < (n + in_page) >> a.shift; j += 256)  // those given up
+    for (u32 j = ((base + (u32)kept + in_page) >> a.shift) + tid; j < (n + in_page) >> a.shift; j += blockDim.x)  // those given up
       if ((u32)table[j] >= a.d.n_pages) wrong |= FDY_ST_BAD_INDEX;
   }
   if (bad) wrong = FDY_ST_BAD_INDEX;
@@ -533,9 +533,10 @@ __global__ void __launch_bounds__(256) keep_plan_kernel(Keep a) {
   plan[1] = n - (u32)drafts, plan[2] = (u32)kept, plan[3] = n;
 }
 
-// A lane takes one 16-byte word of the row's tokens in one plane and moves it for one token after the other, so that a place is
-// read before it is written to: tokens only move to the front.  Eight of them are under way together.
-constexpr u32 kMoved = 8;
+// Where all sources lie behind all places that are written to, every 16-byte word of every token goes by itself, a workgroup
+// kMoved * 256 of a plane's.  Otherwise a lane takes one word of the row's tokens in one plane and moves it for one token after
+// the other, so that a place is read before it is written to: tokens only move to the front.  kSerial of them are under way together.
+constexpr u32 kMoved = 4, kSerial = 16;
 __global__ void __launch_bounds__(256) keep_move_kernel(Keep a) {
   const u32 i = blockIdx.x;
   const u32* plan = a.ws + 4 * i;
@@ -544,21 +545,56 @@ __global__ void __launch_bounds__(256) keep_move_kernel(Keep a) {
   const u32 r = (u32)a.rows[i], in_page = a.d.page_tokens - 1;
   const int32_t *table = a.d.table + (u64)r * a.d.row_pages, *keep = a.keep + (u64)i * a.most;
   const u32 words = a.t.piece_bytes / 16;
-  const u64 all = (u64)a.columns * a.d.n_planes;
-  for (u64 c = blockIdx.y * 256 + threadIdx.x; begin < kept && c < all; c += gridDim.y * 256) {
-    const u32 plane = (u32)(c / a.columns), at = (u32)(c - (u64)plane * a.columns), piece = at / words;
-    uint8_t* const of = (uint8_t*)a.d.planes[plane] + piece * a.t.piece_stride + (at - piece * words) * 16;
-    auto place = [&](u32 token) {
-      return (v4u32*)(of + (u32)table[token >> a.shift] * a.d.page_stride + (token & in_page) * a.t.token_stride);
-    };
-    for (u32 j0 = begin; j0 < kept; j0 += kMoved) {
+  auto place = [&](u64 plane, u32 token, u32 piece, u32 word) {
+    return (v4u32*)((uint8_t*)plane + (u32)table[token >> a.shift] * a.d.page_stride + (token & in_page) * a.t.token_stride +
+                    piece * a.t.piece_stride + word * 16);
+  };
+  if (begin < kept && a.d.n_planes && (u32)keep[begin] >= kept) {
+    const u32 moves = kept - begin;
+    const u64 of_plane = (u64)moves * a.columns;
+    const u32 chunks = (u32)((of_plane + kMoved * 256 - 1) / (kMoved * 256));
+    for (u64 c = blockIdx.y; c < (u64)chunks * a.d.n_planes; c += gridDim.y) {
+      const u32 plane_no = (u32)(c / chunks);
+      const u64 plane = a.d.planes[plane_no], at0 = (c - (u64)plane_no * chunks) * (kMoved * 256) + threadIdx.x;
       v4u32 x[kMoved];
+      v4u32* to[kMoved];
 #pragma unroll
-      for (u32 j = 0; j < kMoved; ++j)
-        if (j0 + j < kept) x[j] = *place(base + (u32)keep[j0 + j]);
+      for (u32 k = 0; k < kMoved; ++k) {
+        const u64 at = at0 + k * 256;
+        to[k] = nullptr;
+        if (at >= of_plane) continue;
+        // neighbouring lanes take what lies side by side: a token's pieces, or a piece's tokens
+        u32 token, piece, word;
+        if (a.t.pieces == 1 || a.t.piece_stride < a.t.token_stride) {
+          token = (u32)(at / a.columns);
+          const u32 rest = (u32)(at - (u64)token * a.columns);
+          piece = rest / words, word = rest - piece * words;
+        } else {
+          const u32 of_piece = moves * words;  // below 2^31: `columns` is no less
+          piece = (u32)(at / of_piece);
+          const u32 rest = (u32)(at - (u64)piece * of_piece);
+          token = rest / words, word = rest - token * words;
+        }
+        x[k] = __builtin_nontemporal_load(place(plane, base + (u32)keep[begin + token], piece, word));
+        to[k] = place(plane, base + begin + token, piece, word);
+      }
 #pragma unroll
-      for (u32 j = 0; j < kMoved; ++j)
-        if (j0 + j < kept) *place(base + j0 + j) = x[j];
+      for (u32 k = 0; k < kMoved; ++k)
+        if (to[k]) __builtin_nontemporal_store(x[k], to[k]);
+    }
+  } else {
+    const u64 all = (u64)a.columns * a.d.n_planes;
+    for (u64 c = blockIdx.y * 256 + threadIdx.x; begin < kept && c < all; c += gridDim.y * 256) {
+      const u32 plane = (u32)(c / a.columns), at = (u32)(c - (u64)plane * a.columns), piece = at / words, word = at - piece * words;
+      for (u32 j0 = begin; j0 < kept; j0 += kSerial) {
+        v4u32 x[kSerial];
+#pragma unroll
+        for (u32 j = 0; j < kSerial; ++j)
+          if (j0 + j < kept) x[j] = *place(a.d.planes[plane], base + (u32)keep[j0 + j], piece, word);
+#pragma unroll
+        for (u32 j = 0; j < kSerial; ++j)
+          if (j0 + j < kept) *place(a.d.planes[plane], base + j0 + j, piece, word) = x[j];
+      }
     }
   }
   if (blockIdx.y) return;
@@ -810,10 +846,12 @@ extern "C" int fdy_pages_keep(const fdy_pages* h, const fdy_token* h_token, cons
   a.n = n, a.most = most;
   a.shift = log2_of(h->page_tokens);
   a.columns = h->n_planes ? t.pieces * (t.piece_bytes / 16) : 0;
-  rc = go(keep_plan_kernel, dim3(n), 256, stream, a);
+  rc = go(keep_plan_kernel, dim3(n), most > 256 ? 1024 : 256, stream, a);
   if (rc != FDY_OK) return rc;
-  const u64 blocks = ((u64)a.columns * h->n_planes + 255) / 256;
-  return go(keep_move_kernel, dim3(n, at_most(blocks + (blocks == 0), 1024)), 256, stream, a);
+  // (how many tokens move is not known here)
+  const u64 blocks = (((u64)most * a.columns + kMoved * 256 - 1) / (kMoved * 256)) * h->n_planes;
+  const u32 y = at_most(blocks + (blocks == 0), 32768 / n < 512 ? 512 : 32768 / n);
+  return go(keep_move_kernel, dim3(n, y), 256, stream, a);
 }
 
 extern "C" int fdy_pages_copy(const fdy_pages* h, const int32_t* d_src, const int32_t* d_dst, uint32_t n,

@@ -5,6 +5,8 @@
 // summed over the query heads of a cache head that is sum_d high_d up_d + low_d down_d with the sums of the positive and of the
 // negative elements: one product of 2 head_dim elements for each page, however many query heads there are.  Bounds are read
 // once, two operations an element: memory bounds it.
+#include <type_traits>
+
 #include "fdy_types.hpp"
 
 using namespace fdy;
@@ -164,91 +166,252 @@ __device__ __forceinline__ double plus_dpp(double x) {
   return x + __builtin_bit_cast(double, dpp<kCtrl, kRows>(v, (u64)0));
 }
 
-// The element of q (type of the queries) as 64 bits.
-template <typename T>
-__device__ __forceinline__ double element(const void* q, u64 at) {
-  return (double)(float)((const typename T::elem*)q)[at];
+// A row's pages in chunks, for each block of heads one after the other: a line through all rows that have more pages than are
+// chosen, of which every workgroup takes an equal share, whatever the rows' lengths are.
+constexpr u32 kPages = 8;           // of a wave, under way together
+constexpr u32 kChunk = 4 * kPages;  // of a workgroup
+template <int kType>
+constexpr u32 kResident = kType == FDY_F8 ? 2 : 4;  // workgroups of a compute unit
+struct Place {
+  u32 s, row, pages, chunks, block, chunk;
+};
+
+// The row of a sequence, in units of the line.
+__device__ __forceinline__ u32 units_of(const Select& a, u32 s, u32& row, u32& pages, bool& bad) {
+  pages = (tokens_of(a.d, s, a.shift, row, bad) + a.d.kv.page_tokens - 1) >> a.shift;
+  return pages > a.d.budget ? (pages + kChunk - 1) / kChunk * a.head_blocks : 0;
+}
+__device__ __forceinline__ void go_to(const Select& a, u32 s, u32 unit, Place& p) {
+  bool bad = false;
+  p.s = s;
+  units_of(a, s, p.row, p.pages, bad);
+  p.row = uniform(p.row), p.pages = uniform(p.pages);
+  p.chunks = (p.pages + kChunk - 1) / kChunk, p.block = unit / p.chunks, p.chunk = unit - p.block * p.chunks;
 }
 
-// A wave takes 64 / lanes heads and every fourth page of the workgroup's.  A lane's 8 (16) factors stay in registers.
-constexpr u32 kPages = 8;           // of a wave, loads under way together
-constexpr u32 kChunk = 4 * kPages * 2;  // pages of a workgroup
-template <typename T, int kType>
-__global__ void __launch_bounds__(256) scores_kernel(Select a) {
-  constexpr int kE = kElems<kType>;
-  constexpr u32 kEs = kType == FDY_F8 ? 1 : 2;
-  const u32 s = blockIdx.x, H = a.d.kv.n_heads, D = a.d.kv.head_dim, wave = threadIdx.x >> 6, l = lane_id();
+// All threads of a workgroup of four waves: its first unit, and how many.
+__device__ __forceinline__ u32 find_units(const Select& a, Place& p) {
+  __shared__ u64 s_sum[4];
+  __shared__ u32 s_seq, s_unit;
+  const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + 255) / 256, s0 = min(tid * slice, n), s1 = min(s0 + slice, n);
+  u64 mine = 0;
   bool bad = false;
-  u32 row;
-  const u32 n = uniform(tokens_of(a.d, s, a.shift, row, bad)), pages = (n + a.d.kv.page_tokens - 1) >> a.shift;
-  if (bad && blockIdx.y == 0 && threadIdx.x == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
-  if (pages <= a.d.budget) return;
-  bad = false;
-  const u32 chunks = (pages + kChunk - 1) / kChunk;
-  u32 last_block = ~0u;
-  double f[kE];
-  for (u32 b = blockIdx.y; b < chunks * a.head_blocks; b += gridDim.y) {
-    const u32 block = b % a.head_blocks, chunk = b / a.head_blocks;
-    const u32 head = block * (64 / a.lanes) + l / a.lanes, piece = l & (a.lanes - 1);
-    const bool works = head < H && piece * kE < 2 * D;
-    const bool high = piece * kE >= D;
-    if (block != last_block) {
-      last_block = block;
+  u32 row, pages;
+  for (u32 s = s0; s < s1; ++s) mine += units_of(a, s, row, pages, bad);
+  if (bad && blockIdx.x == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
+  const u64 inc = wave_incl_scan(mine);
+  if (lane_id() == 63) s_sum[tid >> 6] = inc;
+  __syncthreads();
+  u64 before = inc - mine, total = 0;
 #pragma unroll
-      for (int i = 0; i < kE; ++i) f[i] = 0;
-      if (works) {
-        const double k_scale = kType == FDY_F8 && a.d.kv.k_scale ? (double)a.d.kv.k_scale[head] : 1.0;
-        for (u32 g = 0; g < a.group; ++g) {
-          const u64 at = s * a.d.q_seq + (head * a.group + g) * a.d.q_head + piece * kE - (high ? D : 0);
-#pragma unroll
-          for (int i = 0; i < kE; ++i) {
-            const double x = element<T>(a.d.q, at + i) * k_scale;
-            if (high ? x > 0 : x < 0) f[i] += x;
-          }
-        }
-      }
+  for (u32 w = 0; w < 4; ++w) {
+    if (w < tid >> 6) before += s_sum[w];
+    total += s_sum[w];
+  }
+  const u64 per = (total + gridDim.x - 1) / gridDim.x, begin = blockIdx.x * per;
+  if (begin >= total) return 0;
+  if (begin >= before && begin < before + mine) {
+    u32 s = s0;
+    u64 at = begin - before;
+    for (;; ++s) {
+      const u32 units = units_of(a, s, row, pages, bad);
+      if (at < units) break;
+      at -= units;
     }
-    for (u32 p0 = chunk * kChunk + wave * kPages; p0 < min(pages, (chunk + 1) * kChunk); p0 += 4 * kPages) {
-      v4u32 w[kPages];
-      bool none[kPages];
+    s_seq = s, s_unit = (u32)at;
+  }
+  __syncthreads();
+  go_to(a, uniform(s_seq), uniform(s_unit), p);
+  return (u32)min(per, total - begin);
+}
+
+// A wave's pages of a chunk: their numbers, looked up by scalar loads, and their bounds.
+struct Pages {
+  u32 page[kPages];
+  __device__ __forceinline__ void load(const Select& a, const Place& p, u32 wave) {
+    typedef const __attribute__((address_space(4))) u32* table_t;  // no one writes it while the kernel runs
+    const table_t table = (table_t)(uintptr_t)(a.d.table + (u64)p.row * a.d.row_pages);
 #pragma unroll
-      for (u32 i = 0; i < kPages; ++i) {
-        const u32 j = min(p0 + i, pages - 1), page = (u32)a.d.table[(u64)row * a.d.row_pages + j];
-        none[i] = page >= a.d.kv.n_pages;
-        w[i] = 0;
-        if (works && !none[i]) w[i] = *(const v4u32*)((const uint8_t*)a.d.bounds + ((u64)page * H + head) * 2 * D * kEs + piece * 16);
-      }
+    for (u32 i = 0; i < kPages; ++i) page[i] = table[min(p.chunk * kChunk + wave * kPages + i, p.pages - 1)];
+  }
+};
+template <int kType>
+struct Chunk {
+  v4u32 w[kPages];
+  u32 none;  // bits of pages that are none
+  __device__ __forceinline__ void load(const Select& a, const Pages& p, u32 head, u32 at) {
+    const u32 H = a.d.kv.n_heads, of_head = 2 * a.d.kv.head_dim * (kType == FDY_F8 ? 1 : 2);
+    none = 0;
 #pragma unroll
-      for (u32 i = 0; i < kPages; ++i) {
-        float x[kE];
-        widen<kType>(w[i], x);
-        double sum = 0;
-#pragma unroll
-        for (int k = 0; k < kE; ++k) sum += f[k] != 0 ? f[k] * (double)x[k] : 0.0;
-        sum = plus_dpp<kShr1>(sum);
-        if (a.lanes > 2) sum = plus_dpp<kShr2>(sum);
-        if (a.lanes > 4) sum = plus_dpp<kShr4>(sum);
-        if (a.lanes > 8) sum = plus_dpp<kShr8>(sum);
-        if (a.lanes > 16) sum = plus_dpp<kOfRow, 0xa>(sum);
-        if (a.lanes > 32) sum = plus_dpp<kOfHalf, 0xc>(sum);
-        if (none[i] && p0 + i < pages) bad = true;
-        if (head < H && piece == a.lanes - 1 && p0 + i < pages)
-          a.keys[((u64)s * H + head) * a.d.row_pages + p0 + i] = none[i] ? kNoKey : key_of(sum);
-      }
+    for (u32 i = 0; i < kPages; ++i) {
+      if (p.page[i] >= a.d.kv.n_pages) none |= 1u << i;
+      w[i] = 0;
+      if (head < H && at < of_head && p.page[i] < a.d.kv.n_pages)
+        w[i] = *(const v4u32*)((const uint8_t*)a.d.bounds + ((u64)p.page[i] * H + head) * of_head + at);
     }
   }
-  if (bad) raise_status(a.status, FDY_ST_BAD_INDEX);
+};
+
+// Sums over a group of lanes.  From 16 lanes on of four pages at once: neighbours exchange what they do not go on with, so that lane
+// l has page l % 4 of its four, then the fours are added; the sum that counts, of lanes 12 to 15 of each 16, is formed in the same
+// order for every page.  Smaller groups: of one page, the last lane's counts.
+__device__ __forceinline__ double choose(bool c, double x, double y) { return c ? x : y; }
+__device__ __forceinline__ double sum4(double x0, double x1, double x2, double x3, u32 lanes) {
+  const u32 l = lane_id();
+  const bool odd = l & 1, two = l & 2;
+  constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kRor4 = 0x124, kRor8 = 0x128;
+  auto from = [](auto ctrl, double x) {
+    return __builtin_bit_cast(double, dpp<decltype(ctrl)::value>(__builtin_bit_cast(u64, x), (u64)0));
+  };
+  const double p = choose(odd, x1, x0) + from(std::integral_constant<int, kXor1>(), choose(odd, x0, x1));
+  const double q = choose(odd, x3, x2) + from(std::integral_constant<int, kXor1>(), choose(odd, x2, x3));
+  double r = choose(two, q, p) + from(std::integral_constant<int, kXor2>(), choose(two, p, q));
+  r += from(std::integral_constant<int, kRor4>(), r);
+  r += from(std::integral_constant<int, kRor8>(), r);
+  auto halves = [](auto swap, double x) {
+    const u64 v = __builtin_bit_cast(u64, x);
+    const auto lo = swap((u32)v), hi = swap((u32)(v >> 32));
+    const u32 lo0 = lo[0], lo1 = lo[1], hi0 = hi[0], hi1 = hi[1];
+    return __builtin_bit_cast(double, pair64(lo0, hi0)) + __builtin_bit_cast(double, pair64(lo1, hi1));
+  };
+  if (lanes > 16) r = halves([](u32 v) { return __builtin_amdgcn_permlane16_swap(v, v, false, false); }, r);
+  if (lanes > 32) r = halves([](u32 v) { return __builtin_amdgcn_permlane32_swap(v, v, false, false); }, r);
+  return r;
+}
+__device__ __forceinline__ double sum1(double x, u32 lanes) {
+  x = plus_dpp<kShr1>(x);
+  if (lanes > 2) x = plus_dpp<kShr2>(x);
+  if (lanes > 4) x = plus_dpp<kShr4>(x);
+  return x;
+}
+
+// A wave takes 64 / lanes heads and kPages pages at a time, the next ones asked for ahead.  A lane's 8 (16) factors stay in
+// registers, in 64 bits; where one is 0 the element is made 0, whatever it is.
+template <typename T, int kType>
+__global__ void __launch_bounds__(256, kResident<kType>) scores_kernel(Select a) {
+  constexpr int kE = kElems<kType>, kQ = T::kType;
+  __shared__ double s_f[4][kE][64];
+  const u32 H = a.d.kv.n_heads, D = a.d.kv.head_dim, wave = uniform(threadIdx.x >> 6), l = lane_id();
+  const u32 piece = l & (a.lanes - 1), of_block = 64 / a.lanes, in_block = l / a.lanes;
+  const bool high = piece * kE >= D;
+  Place p;
+  u32 units = find_units(a, p);
+  if (!units) return;
+  // the bounds of the next unit are asked for ahead of this one's sums, and the page numbers of the one behind it
+  auto follow = [&](Place& p) {
+    if (++p.chunk < p.chunks) return;
+    p.chunk = 0;
+    if (++p.block < a.head_blocks) return;
+    u32 s = p.s, row, pages;
+    bool bad = false;
+    do ++s;
+    while (s < a.d.n_seqs && !uniform(units_of(a, s, row, pages, bad)));
+    if (s < a.d.n_seqs) go_to(a, s, 0, p);
+  };
+  Pages pages;
+  pages.load(a, p, wave);
+  Chunk<kType> now;
+  now.load(a, pages, p.block * of_block + in_block, piece * 16);
+  Place then = p;
+  if (units > 1) follow(then), pages.load(a, then, wave);
+  u32 last_s = ~0u, last_block = 0;
+  double f[kE];
+  v4u32 keep = 0;
+  for (;;) {
+    const u32 head = p.block * of_block + in_block;
+    if (p.s != last_s || p.block != last_block) {
+      last_s = p.s, last_block = p.block;
+      keep = 0;
+#pragma unroll
+      for (int i = 0; i < kE; ++i) f[i] = 0;
+      if (head < H && piece * kE < 2 * D) {  // a wave every fourth query head, two of them asked for at once
+        const double k_scale = kType == FDY_F8 && a.d.kv.k_scale ? (double)a.d.kv.k_scale[head] : 1.0;
+        const char* q = (const char*)a.d.q + (p.s * a.d.q_seq + head * a.group * a.d.q_head + piece * kE - (high ? D : 0)) * 2;
+        for (u32 g = wave; g < a.group; g += 8) {
+          v4u32 y[2][kE / 8];
+#pragma unroll
+          for (u32 k = 0; k < 2; ++k)
+#pragma unroll
+            for (int h = 0; h < kE / 8; ++h) {
+              y[k][h] = 0;
+              if (g + 4 * k < a.group) y[k][h] = *(const v4u32*)(q + ((g + 4 * k) * a.d.q_head + h * 8) * 2);
+            }
+#pragma unroll
+          for (u32 k = 0; k < 2; ++k)
+#pragma unroll
+            for (int h = 0; h < kE / 8; ++h) {
+              float z[8];
+              widen<kQ>(y[k][h], z);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const double x = (double)z[i] * k_scale;
+                f[h * 8 + i] += (high ? x > 0 : x < 0) ? x : 0.0;
+              }
+            }
+        }
+      }
+      __syncthreads();  // the sums before have been read
+#pragma unroll
+      for (int i = 0; i < kE; ++i) s_f[wave][i][l] = f[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kE; ++i) {
+        f[i] = s_f[0][i][l] + s_f[1][i][l] + (s_f[2][i][l] + s_f[3][i][l]);
+        if (f[i] != 0) keep[i / (kE / 4)] |= (kType == FDY_F8 ? 0xffu : 0xffffu) << i % (kE / 4) * (32 / (kE / 4));
+      }
+    }
+    const Place at = p;
+    Chunk<kType> next;
+    if (--units) {
+      next.load(a, pages, then.block * of_block + in_block, piece * 16);
+      p = then;
+      if (units > 1) follow(then), pages.load(a, then, wave);
+    }
+    const u32 p0 = at.chunk * kChunk + wave * kPages;
+    double sum[kPages];
+#pragma unroll
+    for (u32 i = 0; i < kPages; ++i) {
+      float x[kE];
+      widen<kType>(now.w[i] & keep, x);
+      sum[i] = 0;
+#pragma unroll
+      for (int k = 0; k < kE; ++k) sum[i] = __builtin_fma(f[k], (double)x[k], sum[i]);
+    }
+    u64* keys = a.keys + ((u64)at.s * H + head) * a.d.row_pages + p0;
+    if (a.lanes >= 16) {
+#pragma unroll
+      for (u32 i = 0; i < kPages; i += 4) {
+        const u64 key = key_of(sum4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3], a.lanes));
+        const u32 mine = i + (l & 3);
+        if (head < H && piece >= 12 && piece < 16 && p0 + mine < at.pages) keys[mine] = now.none >> mine & 1 ? kNoKey : key;
+      }
+    } else {
+#pragma unroll
+      for (u32 i = 0; i < kPages; ++i) {
+        const u64 key = key_of(sum1(sum[i], a.lanes));
+        if (head < H && piece == a.lanes - 1 && p0 + i < at.pages) keys[i] = now.none >> i & 1 ? kNoKey : key;
+      }
+    }
+    if (now.none && l == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
+    if (!units) return;
+    now = next;
+  }
 }
 
 // ---- choice -----------------------------------------------------------------------------------------
 // One workgroup for a cache head of a sequence: the key that the last one taken has, eight bits at a time from the highest in which
 // the keys differ, then those above it and as many of those equal to it as there is room for, in the order of the row.
-constexpr u32 kThreads = 1024;
+// kMine: keys that a thread holds in registers, every kThreads-th of the row; 0: keys are read again from the workspace, for rows of
+// more pages.
+constexpr u32 kThreads = 512, kWaves = kThreads / 64, kBits = 10, kBins = 1u << kBits;
+template <u32 kMine>
 __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
-  __shared__ u64 s_scan[17];
-  __shared__ u64 s_low[16], s_high[16];
-  __shared__ u32 s_bins[256], s_bin, s_above, s_here;
+  __shared__ u64 s_low, s_high, s_scan[17];
+  __shared__ alignas(16) u32 s_bins[2][kBins];
+  __shared__ u32 s_bin, s_above, s_here, s_ranks[kMine * kWaves + 1];
+  __shared__ u64 s_words[kMine * kWaves + 1];
   const u32 H = a.d.kv.n_heads, s = blockIdx.x / H, g = blockIdx.x % H, tid = threadIdx.x, budget = a.d.budget;
+  const u32 wave = tid >> 6, l = lane_id();
   bool bad = false;
   u32 row;
   const u32 n = uniform(tokens_of(a.d, s, a.shift, row, bad)), pages = (n + a.d.kv.page_tokens - 1) >> a.shift;
@@ -266,58 +429,136 @@ __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
     return;
   }
   const u32 sinks = a.d.sinks, recent = a.d.recent, end = pages - recent;
+  u32 left = budget - sinks - recent;  // to be taken of [sinks, end), which are more
+  const u64* keys = a.keys + (u64)blockIdx.x * a.d.row_pages;
+  u64 mine[kMine ? kMine : 1];
+#pragma unroll
+  for (u32 i = 0; i < kMine; ++i) {
+    const u32 j = sinks + i * kThreads + tid;
+    mine[i] = j < end ? keys[j] : 0;
+  }
   for (u32 i = tid; i < sinks; i += kThreads) out[i] = table[i];
   for (u32 i = tid; i < recent; i += kThreads) out[budget - recent + i] = table[end + i];
-  u32 left = budget - sinks - recent;  // to be taken of [sinks, end), which are more
   if (left == 0) return;
-  const u64* keys = a.keys + (u64)blockIdx.x * a.d.row_pages;
-  u64 low = ~0ull, high = 0;
-  for (u32 j = sinks + tid; j < end; j += kThreads) low = min(low, keys[j]), high = max(high, keys[j]);
-  for (u32 m = 1; m < 64; m *= 2) low = min(low, (u64)__shfl_xor((unsigned long long)low, m)), high = max(high, (u64)__shfl_xor((unsigned long long)high, m));
-  if (lane_id() == 0) s_low[tid >> 6] = low, s_high[tid >> 6] = high;
-  __syncthreads();
-  for (u32 w = 0; w < kThreads / 64; ++w) low = min(low, s_low[w]), high = max(high, s_high[w]);
-  // keys from `bound` on, whose bits below `shift` are 0, are `left` and those of its own 2^shift more
-  u32 shift = low == high ? 0 : 64 - (u32)__builtin_clzll(low ^ high);
-  u64 bound = shift == 64 ? 0 : high >> shift << shift;
-  while (shift) {
-    const u32 bits = min(shift, 8u), below = shift - bits;
-    if (tid < 256) s_bins[tid] = 0;
+  auto each = [&](auto f) {  // f(key), of the thread's
+    if constexpr (kMine > 0) {
+#pragma unroll
+      for (u32 i = 0; i < kMine; ++i)
+        if (sinks + i * kThreads < end && sinks + i * kThreads + tid < end) f(mine[i]);
+    } else {
+      for (u32 j = sinks + tid; j < end; j += kThreads) f(keys[j]);
+    }
+  };
+  auto ranks_ahead = [&] {  // s_ranks, each the sum of those ahead of it
     __syncthreads();
-    for (u32 j = sinks + tid; j < end; j += kThreads) {
-      const u64 key = keys[j];
-      if (shift == 64 || key >> shift == bound >> shift) atomicAdd(&s_bins[(u32)(key >> below) & ((1u << bits) - 1)], 1u);
+    constexpr u32 kOf = (kMine * kWaves + 63) / 64;
+    if (wave == 0) {
+      u32 c[kOf + 1], sum = 0;
+#pragma unroll
+      for (u32 i = 0; i < kOf; ++i) c[i] = s_ranks[l * kOf + i], sum += c[i];
+      u32 before = wave_incl_scan(sum) - sum;
+#pragma unroll
+      for (u32 i = 0; i < kOf; ++i) s_ranks[l * kOf + i] = before, before += c[i];
     }
     __syncthreads();
-    if (tid < 64) {  // four bins a lane, from the highest down
-      u32 c[4], sum = 0;
+  };
+  if (tid == 0) s_low = ~0ull, s_high = 0, s_here = end - sinks;
+  for (u32 i = tid; i < 2 * kBins; i += kThreads) s_bins[0][i] = 0;
+  __syncthreads();
+  u64 low = ~0ull, high = 0;
+  each([&](u64 key) { low = min(low, key), high = max(high, key); });
+  low = ~wave_incl_most(~low), high = wave_incl_most(high);
+  if (l == 63) atomicMin((unsigned long long*)&s_low, low), atomicMax((unsigned long long*)&s_high, high);
+  __syncthreads();
+  low = s_low, high = s_high - low;
+  // of the keys less `low` those from `bound` + 2^shift on are taken, and of those from `bound` on `left`
+  u32 shift = high ? 64 - (u32)__builtin_clzll(high) : 0;
+  u64 bound = 0;
+  for (u32 turn = 0; shift; turn ^= 1) {
+    const u32 bits = min(shift, kBits), below = shift - bits;
+    each([&](u64 key) {
+      const u64 x = key - low - bound;  // (those below the bound wrap round)
+      if (shift == 64 || !(x >> shift)) atomicAdd(&s_bins[turn][(u32)(x >> below)], 1u);
+    });
+    __syncthreads();
+    if (wave == 0) {  // kBins / 64 neighbouring bins a lane, the highest in the first
+      constexpr u32 kOf = kBins / 64;
+      u32 c[kOf], sum = 0;
 #pragma unroll
-      for (u32 i = 0; i < 4; ++i) c[i] = s_bins[255 - tid * 4 - i], sum += c[i];
+      for (u32 i = 0; i < kOf; ++i) c[i] = s_bins[turn][(63 - l) * kOf + i], sum += c[i];
       u32 above = wave_incl_scan(sum) - sum;
 #pragma unroll
-      for (u32 i = 0; i < 4; ++i) {
-        if (above < left && above + c[i] >= left) s_bin = 255 - tid * 4 - i, s_above = above, s_here = c[i];
+      for (u32 i = kOf; i-- > 0;) {
+        if (above < left && above + c[i] >= left) s_bin = (63 - l) * kOf + i, s_above = above, s_here = c[i];
         above += c[i];
       }
+    } else {
+      for (u32 i = tid - 64; i < kBins; i += kThreads - 64) s_bins[turn ^ 1][i] = 0;
     }
     __syncthreads();
     left -= s_above;
-    bound |= (u64)s_bin << below;
+    bound += (u64)s_bin << below;
     shift = below;
-    const bool all = s_here == left;
-    __syncthreads();
-    if (all) break;  // all that have these bits are taken
+    if (s_here == left) break;  // all that have these bits are taken
   }
-  u64 before = 0;  // those above in the low half, those equal in the high
-  for (u32 j0 = sinks; j0 < end; j0 += kThreads) {
-    const u32 j = j0 + tid;
-    const u64 key = j < end ? keys[j] >> shift : 0, at = bound >> shift;
-    const u64 mine = j < end ? (key > at ? 1ull : key == at ? 1ull << 32 : 0) : 0;
-    u64 sum;
-    const u64 rank = before + block_excl_scan(mine, s_scan, sum);
-    before += sum;
-    const u32 equal = (u32)(rank >> 32);
-    if (mine == 1 || (mine && equal < left)) out[sinks + (u32)rank + min(equal, left)] = table[j];
+  // (what the next turn writes to s_bin it writes behind a barrier that all have come to)
+  const bool some = s_here != left;  // of those equal
+  bound += low;
+  const u64 step = shift < 64 ? 1ull << shift : 0, over = bound + step;  // (over 0: behind the last of all keys)
+  auto above = [&](u64 key) { return key >= over && over != 0 && shift < 64; };
+  auto equal = [&](u64 key) { return key >= bound && !above(key); };
+  if constexpr (kMine > 0) {
+    // a bit for each page that is taken, with the sums ahead of each word; then every place of the list looks for its page
+    u32 rank = 0;
+    if (some) {
+#pragma unroll
+      for (u32 i = 0; i < kMine; ++i) {
+        const u32 c = (u32)__popcll(ballot(sinks + i * kThreads + tid < end && equal(mine[i])));
+        if (l == i) rank = c;
+      }
+      if (l < kMine) s_ranks[l * kWaves + wave] = rank;
+      ranks_ahead();
+    }
+    u64 word = 0;
+#pragma unroll
+    for (u32 i = 0; i < kMine; ++i) {
+      bool take = sinks + i * kThreads + tid < end && mine[i] >= bound;
+      if (some) {
+        const bool e = take && equal(mine[i]);
+        const u32 at = s_ranks[i * kWaves + wave] + (u32)__popcll(ballot(e) & lanemask_lt());
+        take = take && (!e || at < left);
+      }
+      const u64 taken_here = ballot(take);
+      if (l == i) word = taken_here;
+    }
+    __syncthreads();
+    if (l < kMine) s_words[l * kWaves + wave] = word, s_ranks[l * kWaves + wave] = (u32)__popcll(word);
+    ranks_ahead();
+    for (u32 k = tid; k < budget - sinks - recent; k += kThreads) {
+      u32 at = 0;  // the last word with no more than k ahead of it
+#pragma unroll
+      for (u32 m = kMine * kWaves / 2; m; m /= 2)
+        if (s_ranks[at + m] <= k) at += m;
+      u64 bits = s_words[at];
+      u32 r = k - s_ranks[at], bit = 0;  // its bit number r
+#pragma unroll
+      for (u32 m = 32; m; m /= 2) {
+        const u32 c = (u32)__popcll(bits & ((1ull << m) - 1));
+        if (r >= c) r -= c, bits >>= m, bit += m;
+      }
+      out[sinks + k] = table[sinks + at * 64 + bit];
+    }
+  } else {
+    u64 before = 0;  // those above in the low half, those equal in the high
+    for (u32 j0 = sinks; j0 < end; j0 += kThreads) {
+      const u32 j = j0 + tid;
+      const u64 key = j < end ? keys[j] : 0, x = j < end ? (above(key) ? 1ull : equal(key) ? 1ull << 32 : 0) : 0;
+      u64 sum;
+      const u64 rank = before + block_excl_scan(x, s_scan, sum);
+      before += sum;
+      const u32 equals = (u32)(rank >> 32);
+      if (x == 1 || (x && equals < left)) out[sinks + (u32)rank + min(equals, left)] = table[j];
+    }
   }
 }
 
@@ -394,8 +635,10 @@ extern "C" int fdy_page_select(const fdy_select* h, void* d_workspace, size_t wo
   a.lanes = up_to_power(2 * d.kv.head_dim / (d.kv.type == FDY_F8 ? 16 : 8));
   a.head_blocks = (d.kv.n_heads + 64 / a.lanes - 1) / (64 / a.lanes);
   if (d.row_pages > d.budget) {
-    const u64 blocks = (u64)((d.row_pages + kChunk - 1) / kChunk) * a.head_blocks;
-    const dim3 grid(d.n_seqs, (u32)(blocks < 32768 ? blocks : 32768));
+    // as many workgroups as the card holds (or as there can be units)
+    const u64 units = (u64)d.n_seqs * ((d.row_pages + kChunk - 1) / kChunk) * a.head_blocks;
+    const u64 most = 256 * (d.kv.type == FDY_F8 ? kResident<FDY_F8> : kResident<FDY_BF16>);
+    const dim3 grid((u32)(units < most ? units : most));
     int rc;
     if (d.type == FDY_BF16)
       rc = d.kv.type == FDY_F8 ? go(scores_kernel<Bf16, FDY_F8>, grid, 256, stream, a) : go(scores_kernel<Bf16, FDY_BF16>, grid, 256, stream, a);
@@ -403,5 +646,9 @@ extern "C" int fdy_page_select(const fdy_select* h, void* d_workspace, size_t wo
       rc = d.kv.type == FDY_F8 ? go(scores_kernel<F16, FDY_F8>, grid, 256, stream, a) : go(scores_kernel<F16, FDY_F16>, grid, 256, stream, a);
     if (rc != FDY_OK) return rc;
   }
-  return go(choice_kernel, dim3(d.n_seqs * d.kv.n_heads), kThreads, stream, a);
+  const dim3 grid(d.n_seqs * d.kv.n_heads);
+  if (d.row_pages <= kThreads * 4) return go(choice_kernel<4>, grid, kThreads, stream, a);
+  if (d.row_pages <= kThreads * 16) return go(choice_kernel<16>, grid, kThreads, stream, a);
+  if (d.row_pages <= kThreads * 32) return go(choice_kernel<32>, grid, kThreads, stream, a);
+  return go(choice_kernel<0>, grid, kThreads, stream, a);
 }

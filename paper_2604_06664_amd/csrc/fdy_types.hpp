@@ -13,10 +13,12 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 struct Bf16 {
   typedef __bf16 elem;
   typedef bf16x8 x8;
+  static constexpr int kType = FDY_BF16;
 };
 struct F16 {
   typedef _Float16 elem;
   typedef f16x8 x8;
+  static constexpr int kType = FDY_F16;
 };
 
 constexpr float kF8Most = 448.f;  // largest finite e4m3
