@@ -189,8 +189,8 @@ int fdy_paged_attention(const fdy_attend* h_desc, void* d_workspace, size_t work
  *   at most 64 (0 with sees NULL); max_draft <= 1,024, n_tokens <= 2^23, n_tokens * n_q_heads <= 2^26, n_seqs <= 65,536; with first NULL
  *   n_seqs * max_draft <= n_tokens; row_pages * page_tokens < 2^31; n_seqs * kv.n_heads * (ceil(max_draft * n_q_heads /
  *   kv.n_heads / 16)) * (row_pages * page_tokens / 32 + 5) < 2^31.
- *   workspace  as fdy_paged_attention's: cleared once, left cleared; one sized for a descriptor serves every one with the
- *              same heads, head_dim, page_tokens and kv.type. */
+ *   workspace  device, 256-byte aligned, fdy_tree_attention_workspace_bytes(), contents irrelevant; calls that share one must
+ *              not overlap in time.  One sized for a descriptor serves every one with the same head_dim. */
 typedef struct {
   const void* q;        /* [n_tokens][n_q_heads][head_dim] */
   void* out;            /* [n_tokens][n_q_heads][head_dim] */

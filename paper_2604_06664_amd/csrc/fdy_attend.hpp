@@ -207,10 +207,15 @@ struct Tile {
     }
   }
 
-  // The pages of tokens [t, t + 32): the wave's two, looked up by scalar loads a tile ahead.  ~0: none to be seen
+  // The pages of tokens [t, t + 32): the wave's two, looked up by scalar loads a tile ahead.  ~0: none to be seen.  Small pages: bits
+  // of the half's tokens that are there, once its keys have been asked for
   struct Ids {
     u32 page[2];
   };
+  // All 32 tokens' pages (not the tokens) are there
+  static __device__ __forceinline__ bool whole(const Ids& ids) {
+    return kSmall ? (ids.page[0] & ids.page[1]) == 0xffffu : ids.page[0] != ~0u && ids.page[1] != ~0u;
+  }
   template <typename A>
   static __device__ __forceinline__ Ids ids(const A& a, const Span& span, u32 t, bool& bad) {
     Ids r;
@@ -256,12 +261,13 @@ struct Tile {
 
   // Keys, then values of tokens [t, t + 32); those outside the span read as zero (so do all, at a `t` behind it).
   template <typename A>
-  __device__ __forceinline__ void load_k(const A& a, const Lanes& z, const Span& span, const Ids& ids, u32 t, bool& bad) {
+  __device__ __forceinline__ void load_k(const A& a, const Lanes& z, const Span& span, Ids& ids, u32 t, bool& bad) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const u32 tk = t + u * 16 + z.col;
       if (kSmall) {
         const uint8_t* p = small(a, z, span, tk, a.d.kv.k, bad);
+        ids.page[u] = (u32)ballot(p != nullptr) & 0xffffu;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
           k[u][j] = 0;
@@ -301,10 +307,8 @@ struct Tile {
   // Whether the lane's score i of half u (token t + 16 u + 4 grp + i) has a key.
   template <typename A>
   __device__ __forceinline__ bool seen(const A& a, const Lanes& z, const Span& span, const Ids& ids, u32 t, int u, int i) const {
-    const u32 tok = t + u * 16 + z.grp * 4 + i;
-    const bool in = tok - span.first < span.end - span.first;
-    if (!kSmall) return in && ids.page[u] != ~0u;
-    return in && (u32)a.d.table[(u64)span.row * a.d.row_pages + (tok >> a.page_shift)] < a.d.kv.n_pages;
+    if (kSmall) return ids.page[u] >> (z.grp * 4 + i) & 1;
+    return t + u * 16 + z.grp * 4 + i - span.first < span.end - span.first && ids.page[u] != ~0u;
   }
 
   __device__ x8 key(int u, int step) const {

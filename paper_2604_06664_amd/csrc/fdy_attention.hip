@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) attend_ke
       x.load_v(a, z, span, ids, t, bad);
       for (; t < t_end; t += t_step) {
         const u32 t_next = t + t_step < t_end ? t + t_step : 0x7fffffc0u;  // behind every row
-        const typename Tl::Ids ids_next = Tl::ids(a, span, t_next, bad);
+        typename Tl::Ids ids_next = Tl::ids(a, span, t_next, bad);
         f32x4 s[kTiles][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {

@@ -7,53 +7,63 @@
 // What a row sees differs only in the row's last c tokens (and where a window begins): tiles elsewhere need no masks.  Where
 // rows see different tokens, a value that is no number would come out of the product with weight 0 as NaN in rows that do not see it;
 // such values are taken out of the product and added to the rows that see them one by one.
+#include <type_traits>
+
 #include "fdy_attend.hpp"
 
 using namespace fdy;
 
 namespace {
 
+// A unit of work (below) in parts: where it is, and its parts.  0 of them: none.
+struct Split {
+  u32 parts, seq, unit, second;  // second: the first part lies in the second place of its share
+};
+
 struct TreeArg {
   fdy_draft d;
   u32* status;
-  u32* counters;  // [shares], zero between calls; a unit in parts has its first share's
-  float* parts;   // [shares][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
+  struct Split* splits;  // [shares]: of the unit that goes on from the share to the next
+  float* parts;          // [shares][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
   u32 page_shift, group;
+  u32 beside, fill;  // heads of a token that a workgroup takes at least, if there are so many
 };
 typedef Arg<TreeArg> Tree;
 
 // ---- which work a workgroup takes -------------------------------------------------------------------
-// The query rows of a cache head (drafted tokens x query heads, kRows of them a tile) go to `together` waves side by side, as many
-// times as they need (`groups`); the waves that are left over take other tokens: `apart` tiles of 32 tokens a round.
-// A unit is one such group of one cache head of one sequence; units lie one after the other on a line, kEach places and then a place
-// for every round, and equal shares of the line go to the workgroups.  Groups of one cache head, which read the same, are next to
-// each other.
+// The query rows of a cache head (drafted tokens x query heads) are tiles of kRows; all heads' tiles one after the other are the
+// columns of a sequence.  `together` waves take as many columns side by side: all of a head, which read the same, and of neighbouring
+// heads where these lie beside each other in a token; the waves that are left over take other tokens: `apart` tiles of 32 a round.
+// A unit is one such group of columns of one sequence; units lie one after the other on a line, kEach places and then a place for
+// every round, and equal shares of the line go to the workgroups.
 struct Seq {
   Span span;        // tokens that any of its queries sees
   u32 query, count;  // its first drafted token in q, and how many
   int base;         // tokens ahead of them
-  u32 rows, together, groups, rounds;
+  u32 rows, tiles, columns, together, rounds;  // tiles: of a head's rows
   __device__ u32 unit() const { return rounds + kEach; }
+  __device__ u32 places() const { return (columns + together - 1) / together * unit(); }
 };
 __device__ __forceinline__ Seq uniform(const Seq& v) {
   Seq q;
   q.span.first = fdy::uniform(v.span.first), q.span.end = fdy::uniform(v.span.end), q.span.row = fdy::uniform(v.span.row);
   q.span.bad = v.span.bad;
   q.query = fdy::uniform(v.query), q.count = fdy::uniform(v.count), q.base = (int)fdy::uniform((u32)v.base);
-  q.rows = fdy::uniform(v.rows), q.together = fdy::uniform(v.together), q.groups = fdy::uniform(v.groups);
+  q.rows = fdy::uniform(v.rows), q.together = fdy::uniform(v.together), q.tiles = fdy::uniform(v.tiles);
+  q.columns = fdy::uniform(v.columns);
   q.rounds = fdy::uniform(v.rounds);
   return q;
 }
 
-template <u32 kRows, u32 kWaves>
+template <u32 kRows, u32 kWaves, u32 kLeast>
 __device__ __forceinline__ Seq seq_of(const Tree& a, u32 s) {
   Seq q;
   q.span.row = a.d.rows ? (u32)a.d.rows[s] : s;
   q.span.bad = q.span.row >= a.d.n_rows;
   if (q.span.bad) q.span.row = 0;
   int n = q.span.bad ? 0 : a.d.lens[q.span.row];
-  const u32 most = a.d.row_pages << a.page_shift;
-  if (n < 0 || (u32)n > most) q.span.bad = true, n = n < 0 ? 0 : (int)most;
+  const u32 room = a.d.row_pages << a.page_shift;
+  if (n < 0 || (u32)n > room) q.span.bad = true, n = n < 0 ? 0 : (int)room;
   u32 from = s * a.d.max_draft, to = from + a.d.max_draft;
   if (a.d.first) from = (u32)a.d.first[s], to = (u32)a.d.first[s + 1];
   q.query = from, q.count = to - from;
@@ -63,10 +73,14 @@ __device__ __forceinline__ Seq seq_of(const Tree& a, u32 s) {
   q.span.end = q.count ? (u32)n : 0;
   q.span.first = a.d.window && q.base > 0 && (u32)q.base > a.d.window ? (u32)q.base - a.d.window : 0;
   q.rows = q.count * a.group;
-  const u32 tiles = (q.rows + kRows - 1) / kRows;
-  q.together = 1;
-  while (q.together < kWaves && q.together < tiles) q.together *= 2;
-  q.groups = (tiles + q.together - 1) / q.together;
+  q.tiles = (q.rows + kRows - 1) / kRows;
+  q.together = kLeast;
+  const u32 most = kLeast == 1 && a.beside > q.tiles ? a.beside : q.tiles;
+  while (q.together < kWaves && q.together < most) q.together *= 2;
+  if (kLeast > 1) q.tiles = (q.tiles + q.together - 1) / q.together * q.together;  // a group's are of one head
+  q.columns = q.tiles * a.d.kv.n_heads;
+  if (kLeast == 1)
+    while (q.together > 1 && q.together >= 2 * q.columns) q.together /= 2;
   const u32 apart = kWaves / q.together;
   q.rounds = (q.span.tiles() + apart - 1) / apart;
   return q;
@@ -83,15 +97,15 @@ struct TreeLds {
 };
 
 // All threads of the workgroup.
-template <u32 kRows, u32 kWaves>
+template <u32 kRows, u32 kWaves, u32 kLeast>
 __device__ __forceinline__ bool find_tree_share(const Tree& a, TreeShare& out, TreeLds<kWaves>& lds) {
   constexpr u32 kThreads = 64 * kWaves;
   const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + kThreads - 1) / kThreads;
   const u32 s0 = min(tid * slice, n), s1 = min(s0 + slice, n);
   auto cost = [&](u32 s) {
-    const Seq q = seq_of<kRows, kWaves>(a, s);
+    const Seq q = seq_of<kRows, kWaves, kLeast>(a, s);
     if (q.span.bad && q.count == 0 && blockIdx.x == 0) raise_status(a.status, FDY_ST_BAD_INDEX);  // no one else looks at it
-    return a.d.kv.n_heads * q.groups * q.unit();
+    return q.places();
   };
   u32 mine = 0;
   for (u32 s = s0; s < s1; ++s) mine += cost(s);
@@ -105,10 +119,11 @@ __device__ __forceinline__ bool find_tree_share(const Tree& a, TreeShare& out, T
     total += lds.sum[w];
   }
   total = fdy::uniform(total);
-  if (total == 0) return false;
   // dies take workgroups in turn: neighbours on the line, which read the same keys and values, go to one
   const u32 g = gridDim.x;
   out.at = g % 8 ? blockIdx.x : blockIdx.x % 8 * (g / 8) + blockIdx.x / 8;
+  if (tid == 0) a.splits[out.at].parts = 0;
+  if (total == 0) return false;
   out.per = max((total - 1) / g + 1, kEach + 1);
   if ((u64)out.at * out.per >= total) return false;
   out.begin = out.at * out.per;
@@ -188,6 +203,11 @@ __device__ __forceinline__ u32 sees4(const Tree& a, const Seq& q, const View& v,
 }
 
 // ---- values that are no finite numbers --------------------------------------------------------------
+template <typename T>
+constexpr u32 kExponent = 0x7c00u;
+template <>
+inline constexpr u32 kExponent<Bf16> = 0x7f80u;
+
 template <typename T, bool kF8>
 __device__ __forceinline__ u32 odd_mask(u32 w) {  // all bits of each element of the word that is infinite or no number
   if (kF8) {
@@ -197,37 +217,506 @@ __device__ __forceinline__ u32 odd_mask(u32 w) {  // all bits of each element of
       if ((w >> 8 * i & 0x7f) == 0x7f) m |= 0xffu << 8 * i;
     return m;
   }
-  constexpr u32 kExp = sizeof(typename T::elem) == 2 && __is_same(T, Bf16) ? 0x7f80u : 0x7c00u;
-  return ((w & kExp) == kExp ? 0xffffu : 0) | ((w >> 16 & kExp) == kExp ? 0xffff0000u : 0);
+  return ((w & kExponent<T>) == kExponent<T> ? 0xffffu : 0) | ((w >> 16 & kExponent<T>) == kExponent<T> ? 0xffff0000u : 0);
+}
+
+// ---- a wave's sums ----------------------------------------------------------------------------------
+template <typename T, int kDim, int kTiles>
+struct Sums {
+  typedef typename T::x8 x8;
+  f32x4 o[kTiles][kDim / 16];
+  float m[kTiles], sum[kTiles];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int qt = 0; qt < kTiles; ++qt) {
+      m[qt] = -INFINITY, sum[qt] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kDim / 16; ++i) o[qt][i] = 0;
+    }
+  }
+
+  // The weights of a tile's scores, in two parts; the sums so far are brought to the new maximum.
+  __device__ __forceinline__ void weigh(const f32x4 (*s)[2], float scale, x8* p, x8* rest) {
+    float keep[kTiles];
+#pragma unroll
+    for (int qt = 0; qt < kTiles; ++qt) {
+      float mx = s[qt][0][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[qt][j / 4][j % 4]);
+      const float m_new = fmaxf(m[qt], over_groups(mx, larger)), ref = m_new == -INFINITY ? 0.f : m_new;
+      keep[qt] = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
+      m[qt] = m_new;
+      float part = 0.f;
+      v4u32 first_of, rest_of;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4] - ref, scale, kLift<T>));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4 + 1] - ref, scale, kLift<T>));
+        part += e0 + e1;
+        u32 hi_of, lo_of;
+        split<T>(e0, e1, hi_of, lo_of);
+        first_of[j] = hi_of, rest_of[j] = lo_of;
+      }
+      p[qt] = __builtin_bit_cast(x8, first_of), rest[qt] = __builtin_bit_cast(x8, rest_of);
+      sum[qt] = sum[qt] * keep[qt] + part;
+    }
+    // (the maximum moves seldom once some tiles have been seen)
+    bool moved = false;
+#pragma unroll
+    for (int qt = 0; qt < kTiles; ++qt) moved |= keep[qt] != 1.f;
+    if (ballot(moved))
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+        for (int i = 0; i < kDim / 16; ++i) o[qt][i] *= keep[qt];
+  }
+};
+
+// Which of the lane's eight scores of a tile each of its rows sees; those that it does not at minus infinity.
+template <int kTiles>
+__device__ __forceinline__ void show(const Tree& a, const Seq& q, const u32* draft, u32 there, int tok, f32x4 (*s)[2]) {
+#pragma unroll
+  for (int qt = 0; qt < kTiles; ++qt) {
+    const View view = view_of(a, q, draft[qt]);
+    const u32 shown = there & (sees4(a, q, view, tok) | sees4(a, q, view, tok + 16) << 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[qt][j / 4][j % 4] = shown >> j & 1 ? s[qt][j / 4][j % 4] : -INFINITY;
+  }
+}
+
+// The tokens of a tile that a lane's row sees (bit i: token i), from the four lanes that have eight of them each.
+__device__ __forceinline__ u32 tokens_seen(const Tree& a, const Seq& q, const View& v, u32 there, int tok) {
+  const u32 mine = there & (sees4(a, q, v, tok) | sees4(a, q, v, tok + 16) << 4), col = lane_id() & 15;
+  u32 all = 0;
+#pragma unroll
+  for (u32 g = 0; g < 4; ++g) {
+    const u32 of = (u32)__shfl((int)mine, (int)(col + 16 * g));
+    all |= (of & 0xf) << 4 * g | (of >> 4) << (16 + 4 * g);
+  }
+  return all;
+}
+
+// ---- tiles from the pages to registers --------------------------------------------------------------
+// Every wave for itself; the next tile's keys are asked for as soon as this one's are used up, its values likewise.  As in Tile,
+// o[.][part * kWide + e][i] is of element part * 16 * kWide + (4 grp + i) * kWide + e.
+template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles>
+struct Alone {
+  typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
+  typedef typename T::x8 x8;
+  static constexpr int kWide = Tl::kWide, kParts = Tl::kParts, kSteps = Tl::kSteps;
+  static __device__ __forceinline__ u32 element(u32 i, u32 k, u32 grp) {  // of o[.][i][k]
+    return i / kWide * 16 * kWide + (grp * 4 + k) * kWide + i % kWide;
+  }
+
+  static __device__ __forceinline__ void walk(const Tree& a, const Seq& q, const typename Tl::Lanes& z, const x8 (*qs)[kSteps],
+                                              const u32* draft, float scale, u32 t, u32 t_end, u32 t_step,
+                                              Sums<T, kDim, kTiles>& sums, bool& bad) {
+    if (t >= t_end) return;
+    // tiles in which rows see different tokens, or tokens are not there
+    const int past = q.base, opens = a.d.window ? (int)(q.span.end - a.d.window) : 0;
+    Tl x;
+    typename Tl::Ids ids = Tl::ids(a, q.span, t, bad);
+    x.load_k(a, z, q.span, ids, t, bad);
+    x.load_v(a, z, q.span, ids, t, bad);
+    for (; t < t_end; t += t_step) {
+      const u32 t_next = t + t_step < t_end ? t + t_step : 0x7fffffc0u;  // behind every row
+      typename Tl::Ids ids_next = Tl::ids(a, q.span, t_next, bad);
+      f32x4 s[kTiles][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = 0;
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+          const x8 key = x.key(u, st);
+#pragma unroll
+          for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = mfma<T>(key, qs[qt][st], s[qt][u]);
+        }
+      }
+      x.load_k(a, z, q.span, ids_next, t_next, bad);
+      bool odd = false;
+      u32 there = 0;
+      if (!(Tl::whole(ids) && (int)(t + kTile) <= past && (int)t >= opens)) {
+        u32 any = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) there |= x.seen(a, z, q.span, ids, t, j / 4, j % 4) ? 1u << j : 0;
+        show<kTiles>(a, q, draft, there, (int)(t + z.grp * 4), s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int pt = 0; pt < kParts; ++pt)
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(typename Tl::vword) / 4; ++k) {
+              const u32 m = odd_mask<T, kF8>(word(x.v[i][pt], k));
+              any |= m;
+              if constexpr (sizeof(typename Tl::vword) == 4)
+                x.v[i][pt] &= ~m;
+              else
+                x.v[i][pt][k] &= ~m;
+            }
+        odd = ballot(any != 0) != 0;
+      }
+      x8 p[kTiles], rest[kTiles];
+      sums.weigh(s, scale, p, rest);
+#pragma unroll
+      for (int pt = 0; pt < kParts; ++pt)
+#pragma unroll
+        for (int e2 = 0; e2 < kWide / 2; ++e2) {
+          x8 even, odd_e;
+          x.values(pt, e2, even, odd_e);
+#pragma unroll
+          for (int qt = 0; qt < kTiles; ++qt) {
+            f32x4& c0 = sums.o[qt][pt * kWide + 2 * e2];
+            f32x4& c1 = sums.o[qt][pt * kWide + 2 * e2 + 1];
+            c0 = mfma<T>(even, p[qt], c0);
+            c1 = mfma<T>(odd_e, p[qt], c1);
+            c0 = mfma<T>(even, rest[qt], c0);
+            c1 = mfma<T>(odd_e, rest[qt], c1);
+          }
+        }
+      if (odd) {  // the elements that were taken out, to the rows that see them: whatever the weight is, it is not 0
+        u32 seen[kTiles];
+#pragma unroll
+        for (int qt = 0; qt < kTiles; ++qt) seen[qt] = tokens_seen(a, q, view_of(a, q, draft[qt]), there, (int)(t + z.grp * 4));
+        for (u32 i = 0; i < kTile; ++i) {
+          const u32 tok = t + i;
+          if (tok - q.span.first >= q.span.end - q.span.first) continue;
+          const u32 page = (u32)a.d.table[(u64)q.span.row * a.d.row_pages + (tok >> a.page_shift)];
+          if (page >= a.d.kv.n_pages) continue;
+          const uint8_t* from = (const uint8_t*)a.d.kv.v + Tl::place(a, z, page, tok);
+#pragma unroll
+          for (int d = 0; d < kDim / 16; ++d)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const u32 e = element(d, k, z.grp);
+              if (e >= a.d.kv.head_dim) continue;
+              float y;
+              if (kF8)
+                y = (from[e] & 0x7f) == 0x7f ? NAN : 0.f;
+              else
+                y = (float)((const typename T::elem*)from)[e];
+              if (__builtin_isfinite(y)) continue;
+#pragma unroll
+              for (int qt = 0; qt < kTiles; ++qt)
+                if (seen[qt] >> i & 1) sums.o[qt][d][k] += y;
+            }
+        }
+      }
+      x.load_v(a, z, q.span, ids_next, t_next, bad);
+      ids = ids_next;
+    }
+  }
+};
+
+// ---- tiles through shared memory --------------------------------------------------------------------
+// Where several waves take the same tokens, a workgroup reads a tile once: its eight waves bring pieces of 1 KiB of several tiles from
+// the pages to registers, a stage ahead, and from there to LDS (8-bit elements widened on the way), in two slots that take turns.
+// A token's row of kDim elements lies in chunks of 32 bytes, chunk c at c ^ turn(token), so that neither the keys' rows (16 bytes of
+// 16 tokens) nor the values' columns (16 elements of 4 tokens, which the transposing read hands out token by token) meet in a bank.
+// o[.][i][k] is of element 16 i + 4 grp + k.
+//
+// kDirect: straight from the pages to LDS, which 16-bit elements and heads of exactly kDim allow.
+template <typename T, bool kF8, int kDim, int kTiles, bool kDirect, u32 kWaves>
+struct Together {
+  typedef typename T::x8 x8;
+  typedef typename T::elem elem;
+  static constexpr u32 kEs = kF8 ? 1 : 2, kRow = kDim * 2, kTileBytes = 2 * kTile * kRow;  // of keys, then values
+  static constexpr u32 kMost = kWaves / 4;  // tiles of a stage
+  static constexpr u32 kSlot = kMost * kTileBytes;
+  static constexpr int kSteps = kDim / 32;
+  static constexpr u32 kPieces = 2 * kTile * kDim * kEs / 1024, kMine = (kPieces + kWaves - 1) / kWaves;  // of a tile; of a wave
+  static constexpr u32 kLanes = kDim * kEs / 16, kTokens = 64 / kLanes;  // lanes of a token, tokens of a piece
+  static __device__ __forceinline__ u32 element(u32 i, u32 k, u32 grp) { return i * 16 + grp * 4 + k; }
+  static __device__ __forceinline__ u32 turn(u32 token) { return kDim == 64 ? token >> 1 & 3 : token & 7; }
+
+  // Pages of a stage's tiles (0 where a number is none: what comes of it is not looked at).  Tiles that reach over the row's ends take
+  // its first or last page there.
+  struct Ids {
+    u32 page[kMost][2], there;  // there: bits 2 i + u of the halves that have a page
+  };
+  static __device__ __forceinline__ void look_up(const Tree& a, const Seq& q, u32 tile, Ids& ids, bool& bad) {
+    typedef const __attribute__((address_space(4))) u32* table_t;  // no one writes it while the kernel runs
+    const table_t table = (table_t)(uintptr_t)(a.d.table + (u64)q.span.row * a.d.row_pages);
+    const u32 low = q.span.first >> a.page_shift, high = (q.span.end - 1) >> a.page_shift;
+    ids.there = 0;
+#pragma unroll
+    for (u32 i = 0; i < kMost; ++i)
+#pragma unroll
+      for (u32 u = 0; u < 2; ++u) {
+        const u32 j = ((tile + i) * kTile + u * 16) >> a.page_shift;
+        ids.page[i][u] = table[max(low, min(j, high))];
+      }
+#pragma unroll
+    for (u32 i = 0; i < kMost; ++i)
+#pragma unroll
+      for (u32 u = 0; u < 2; ++u) {
+        const bool ok = ids.page[i][u] < a.d.kv.n_pages;
+        ids.there |= ok ? 1u << (2 * i + u) : 0;
+        ids.page[i][u] = ok ? ids.page[i][u] : 0;
+        bad |= !ok;
+      }
+  }
+
+  v4u32 w[kMost][kMine];
+  u32 lane_at[kMine];  // the lane's place in its piece's 16 tokens; kNowhere behind head_dim
+  __device__ __forceinline__ void lanes(const Tree& a, u32 wave) {
+    const u32 l = lane_id(), in = l / kLanes, c = l % kLanes, token_bytes = (u32)a.d.kv.token_stride * kEs;
+#pragma unroll
+    for (u32 m = 0; m < kMine; ++m) {
+      const u32 token = token_of(wave + m * kWaves) + in;
+      // 16-bit: the lane's 16 bytes go to half c % 2 of chunk c / 2; 8-bit: they are a chunk
+      const u32 chunk = (kF8 ? c : c / 2) ^ turn(token), at = kF8 ? chunk * 16 : chunk * 32 + c % 2 * 16;
+      lane_at[m] = at < a.d.kv.head_dim * kEs ? (token & 15) * token_bytes + at : kNowhere;
+    }
+  }
+  static __device__ __forceinline__ u32 token_of(u32 piece) { return piece % (kPieces / 2) * kTokens; }
+  __device__ __forceinline__ void load(const Tree& a, u32 of_head, u32 wave, u32 tile, u32 n, const Ids& ids) {
+    const u64 page_bytes = a.d.kv.page_stride * kEs;
+    const u32 token_bytes = (u32)a.d.kv.token_stride * kEs;
+#pragma unroll
+    for (u32 i = 0; i < kMost; ++i)
+#pragma unroll
+      for (u32 m = 0; m < kMine; ++m) {
+        const u32 piece = wave + m * kWaves, u = token_of(piece) / 16;
+        const u32 page = ids.page[i][0] ^ ((ids.page[i][0] ^ ids.page[i][1]) & (0u - u));
+        const u32 in_page = (((tile + i) * kTile + u * 16) & (a.d.kv.page_tokens - 1)) * token_bytes + of_head;
+        const auto from = buffer((const uint8_t*)(piece >= kPieces / 2 ? a.d.kv.v : a.d.kv.k) + page * page_bytes, kNowhere - 1);
+        w[i][m] = 0;
+        if (i < n && piece < kPieces) w[i][m] = __builtin_amdgcn_raw_buffer_load_b128(from, lane_at[m], in_page, 0);
+      }
+  }
+  // The same to LDS, 1 KiB of it from `slot` on for each piece.  (Written as it stands since the compiler has every later read of LDS wait
+  // for such loads, whichever slot it is of; the workgroup's barrier behind arrived() is what orders them.)
+  __device__ __forceinline__ void bring(const Tree& a, u32 of_head, u32 wave, u32 tile, u32 n, const Ids& ids, u32 slot) const {
+    const u64 page_bytes = a.d.kv.page_stride * kEs;
+    const u32 token_bytes = (u32)a.d.kv.token_stride * kEs;
+#pragma unroll
+    for (u32 i = 0; i < kMost; ++i)
+#pragma unroll
+      for (u32 m = 0; m < kMine; ++m) {
+        const u32 piece = wave + m * kWaves, u = token_of(piece) / 16;
+        const u32 page = ids.page[i][0] ^ ((ids.page[i][0] ^ ids.page[i][1]) & (0u - u));
+        const u32 in_page = (((tile + i) * kTile + u * 16) & (a.d.kv.page_tokens - 1)) * token_bytes + of_head;
+        const u64 from = fdy::uniform((u64)(uintptr_t)(piece >= kPieces / 2 ? a.d.kv.v : a.d.kv.k) + page * page_bytes);
+        const v4u32 rsrc = {(u32)from, (u32)(from >> 32) & 0xffffu, kNowhere - 1, 0x00020000u};
+        const u32 to = fdy::uniform(slot + i * kTileBytes + piece * 1024);
+        if (i < n && piece < kPieces)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                       :
+                       : "s"(to), "v"(lane_at[m]), "s"(rsrc), "s"(fdy::uniform(in_page))
+                       : "memory");
+      }
+  }
+  static __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+  __device__ __forceinline__ void store(uint8_t* slot, u32 wave, u32 n) const {
+    const u32 l = lane_id();
+#pragma unroll
+    for (u32 i = 0; i < kMost; ++i)
+#pragma unroll
+      for (u32 m = 0; m < kMine; ++m) {
+        const u32 piece = wave + m * kWaves;
+        if (i >= n || piece >= kPieces) continue;
+        uint8_t* to = slot + i * kTileBytes + (piece * 64 + l) * (kF8 ? 32 : 16);
+        if constexpr (kF8) {
+          v4u32 lo, hi;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            lo[2 * k] = widen_f8x2<T, false>(w[i][m][k]), lo[2 * k + 1] = widen_f8x2<T, true>(w[i][m][k]);
+            hi[2 * k] = widen_f8x2<T, false>(w[i][m][2 + k]), hi[2 * k + 1] = widen_f8x2<T, true>(w[i][m][2 + k]);
+          }
+          *(v4u32*)to = lo, *(v4u32*)(to + 16) = hi;
+        } else {
+          *(v4u32*)to = w[i][m];
+        }
+      }
+  }
+
+  // Eight tokens of the lane's element of 16 i + ..., as the products take them.
+  static __device__ __forceinline__ x8 value(const uint8_t* v, u32 at, u32 i) {
+    typedef short i16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) i16x4* lds_t;
+    const uint8_t* from = v + (at ^ i * 32);
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)from);
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(from + 16 * kRow));
+    return __builtin_bit_cast(x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+
+  // A tile that lies at `k`.  kPlain: all its rows see all of its tokens.
+  template <bool kPlain>
+  static __device__ __forceinline__ void take(const Tree& a, const Seq& q, const uint8_t* k, u32 t, u32 pages, const x8 (*qs)[kSteps],
+                                              const u32* draft, float scale, Sums<T, kDim, kTiles>& sums) {
+    const u32 l = lane_id(), col = l & 15, grp = l >> 4;
+    const uint8_t* v = k + kTile * kRow;
+    u32 k_at = col * kRow + ((grp >> 1 ^ turn(col)) * 32 + (grp & 1) * 16);
+    const u32 v_token = grp * 4 + (col >> 2);
+    u32 v_at = v_token * kRow + (turn(v_token) * 32 + (col & 3) * 8);
+    asm volatile("" : "+v"(k_at), "+v"(v_at));  // worked out again for each tile: what follows from them would take a dozen registers
+    f32x4 s[kTiles][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = 0;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const x8 key = __builtin_bit_cast(x8, *(const v4u32*)(k + (k_at ^ st * 64) + u * 16 * kRow));
+#pragma unroll
+        for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = mfma<T>(key, qs[qt][st], s[qt][u]);
+      }
+    u32 there = 0, any = 0;
+    if (!kPlain) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const u32 tok = t + (j / 4) * 16 + grp * 4 + j % 4;
+        if (tok - q.span.first < q.span.end - q.span.first && (pages >> (j / 4) & 1)) there |= 1u << j;
+      }
+      show<kTiles>(a, q, draft, there, (int)(t + grp * 4), s);
+    }
+    x8 p[kTiles], rest[kTiles];
+    sums.weigh(s, scale, p, rest);
+#pragma unroll
+    for (int i = 0; i < kDim / 16; ++i) {
+      x8 x = value(v, v_at, i);
+      if (!kPlain) {  // nothing of tokens that are not there, and no infinities
+        v4u32 y = __builtin_bit_cast(v4u32, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y[j] &= (there >> (2 * j) & 1 ? 0xffffu : 0) | (there >> (2 * j + 1) & 1 ? 0xffff0000u : 0);
+          const u32 m = odd_mask<T, false>(y[j]);
+          any |= m;
+          y[j] &= ~m;
+        }
+        x = __builtin_bit_cast(x8, y);
+      }
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) sums.o[qt][i] = mfma<T>(x, p[qt], sums.o[qt][i]);
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) sums.o[qt][i] = mfma<T>(x, rest[qt], sums.o[qt][i]);
+    }
+    if (!kPlain && ballot(any != 0)) {  // what was taken out, to the rows that see it: whatever the weight is, it is not 0
+      u32 seen[kTiles];
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) seen[qt] = tokens_seen(a, q, view_of(a, q, draft[qt]), there, (int)(t + grp * 4));
+      for (u32 token = 0; token < kTile; ++token) {
+        if (t + token - q.span.first >= q.span.end - q.span.first || !(pages >> token / 16 & 1)) continue;
+#pragma unroll
+        for (int i = 0; i < kDim / 16; ++i)
+#pragma unroll
+          for (u32 e = 0; e < 4; ++e) {
+            const float y = (float)*(const elem*)(v + token * kRow + ((i ^ turn(token)) * 32 + (grp * 4 + e) * 2));
+            if (__builtin_isfinite(y)) continue;
+#pragma unroll
+            for (int qt = 0; qt < kTiles; ++qt)
+              if (seen[qt] >> token & 1) sums.o[qt][i][e] += y;
+          }
+      }
+    }
+  }
+
+  // Tiles [tile, end): of each stage's the wave takes those that are its `turn` of `apart`.  All waves of the workgroup.
+  static __device__ __forceinline__ void walk(const Tree& a, const Seq& q, u32 head, const x8 (*qs)[kSteps], const u32* draft, float scale,
+                                              u32 tile, u32 end, u32 apart, u32 mine, bool works, uint8_t* lds, Sums<T, kDim, kTiles>& sums,
+                                              bool& bad) {
+    const u32 wave = fdy::uniform(threadIdx.x >> 6);
+    constexpr u32 step = kMost;
+    const int opens = a.d.window ? (int)(q.span.end - a.d.window) : 0;  // from there on all rows' windows are open
+    auto count = [&](u32 from) { return from >= end ? 0 : end - from < step ? end - from : step; };
+    // page numbers two stages ahead, loads one, so that both are under way while a stage is worked on
+    const u32 of_head = head * (u32)a.d.kv.head_stride * kEs, at = (u32)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    Together x;
+    x.lanes(a, wave);
+    Ids ids;
+    look_up(a, q, tile, ids, bad);
+    if (kDirect)
+      x.bring(a, of_head, wave, tile, count(tile), ids, at);
+    else
+      x.load(a, of_head, wave, tile, count(tile), ids);
+    u32 pages = ids.there, pages_next = 0, slot = 0;
+    look_up(a, q, tile + step, ids, bad);
+    if (!kDirect) {
+      x.store(lds, wave, count(tile));
+      x.load(a, of_head, wave, tile + step, count(tile + step), ids);
+      pages_next = ids.there;
+      look_up(a, q, tile + 2 * step, ids, bad);
+    }
+    // while a stage is worked on the next one is brought to LDS; or that to LDS, the one behind it to registers
+    for (; tile < end; tile += step, slot ^= 1) {
+      if (kDirect) arrived();
+      __syncthreads();  // the slot is filled, the other one read
+      u32 pages_then = 0;
+      if (kDirect) {
+        x.bring(a, of_head, wave, tile + step, count(tile + step), ids, at + (slot ^ 1) * kSlot);
+        pages_next = ids.there;
+        look_up(a, q, tile + 2 * step, ids, bad);
+      } else {
+        x.store(lds + (slot ^ 1) * kSlot, wave, count(tile + step));
+        x.load(a, of_head, wave, tile + 2 * step, count(tile + 2 * step), ids);
+        pages_then = ids.there;
+        look_up(a, q, tile + 3 * step, ids, bad);
+      }
+      const u32 n = count(tile);
+      if (works)
+        for (u32 i = mine; i < n; i += apart) {
+          const u32 t = (tile + i) * kTile, of = pages >> 2 * i & 3;
+          const uint8_t* k = lds + slot * kSlot + i * kTileBytes;
+          if (of == 3 && (int)(t + kTile) <= q.base && (int)t >= opens)
+            take<true>(a, q, k, t, of, qs, draft, scale, sums);
+          else
+            take<false>(a, q, k, t, of, qs, draft, scale, sums);
+        }
+      pages = pages_next, pages_next = pages_then;
+    }
+    __syncthreads();  // what follows goes where the slots lie
+  }
+};
+
+// Elements [d, d + 4) of a head's row, from the sums over all of its tokens.
+template <typename E>
+__device__ __forceinline__ void finish_row(const Tree& a, const Seq& q, u32 kv_head, u32 row, u32 d, float M, float L, f32x4 y) {
+  const u32 j = row / a.group, h = kv_head * a.group + row - j * a.group;
+  const float v_scale = a.d.kv.type == FDY_F8 && a.d.kv.v_scale ? a.d.kv.v_scale[kv_head] : 1.f;
+  y = y * (L == 0.f ? 0.f : v_scale / L);
+  typedef E x4 __attribute__((ext_vector_type(4)));
+  *(x4*)((E*)a.d.out + (u64)(q.query + j) * a.d.out_token + (u64)h * a.d.out_head + d) = __builtin_convertvector(y, x4);
+  if (d == 0 && a.d.lse) a.d.lse[(u64)(q.query + j) * a.d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
 }
 
 // ---- the kernel -------------------------------------------------------------------------------------
-constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; }
+constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; }  // workgroups of a compute unit
+constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves == 4 ? 3 : 1) : resident(dim, waves); }
 
-template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves>
-__global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) tree_kernel(Tree a) {
+// kShared: four waves at least take the same tokens, eight waves a workgroup.
+template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves, bool kShared, bool kDirect>
+__global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) * kWaves / 4) tree_kernel(Tree a) {
   typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
+  typedef Together<T, kF8, kDim, kTiles, kDirect, kWaves> Both;
+  typedef typename std::conditional<kShared, Both, Alone<T, kF8, kDim, kSmall, kPolicy, kTiles>>::type Way;
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
-  constexpr int kWide = Tl::kWide, kParts = Tl::kParts, kSteps = Tl::kSteps, kPad = kDim + 4;
+  constexpr int kSteps = kDim / 32, kPad = kDim + 4;
+  constexpr u32 kLeast = kShared ? 4 : 1;  // so that a stage of two tiles has work for all waves
   constexpr u32 kRows = 16 * kTiles, kThreads = 64 * kWaves;
-  __shared__ alignas(16) float s_o[kWaves][kRows][kPad];
+  constexpr u32 kSumBytes = kWaves * kRows * kPad * 4, kSlotBytes = kShared ? 2 * Both::kSlot : 0;
+  __shared__ alignas(16) uint8_t s_mem[kSumBytes > kSlotBytes ? kSumBytes : kSlotBytes];
+  float(*s_o)[kRows][kPad] = (float(*)[kRows][kPad])s_mem;
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
   __shared__ TreeLds<kWaves> s_share;
-  __shared__ u32 s_last;
 
   TreeShare share;
-  if (!find_tree_share<kRows, kWaves>(a, share, s_share)) return;
-  const u32 wave = fdy::uniform(threadIdx.x >> 6), D = a.d.kv.head_dim, quads = D / 4, H = a.d.kv.n_heads;
+  if (!find_tree_share<kRows, kWaves, kLeast>(a, share, s_share)) return;
+  const u32 wave = fdy::uniform(threadIdx.x >> 6), D = a.d.kv.head_dim, quads = D / 4;
   const u32 part_size = part_floats(kRows * kWaves, D);
+  // parts are written through to memory as they come: what the caches held of them would be written at the kernel's end, by itself
   const auto parts = buffer(a.parts, gridDim.x * 2 * part_size * 4);  // within 2^30 bytes
 
   u32 seq = share.seq, seq_start = share.start;
-  Seq q = uniform(seq_of<kRows, kWaves>(a, seq));
+  Seq q = uniform(seq_of<kRows, kWaves, kLeast>(a, seq));
   for (u32 place = share.begin; place < share.end;) {
-    while (place - seq_start >= H * q.groups * q.unit()) {
-      seq_start += H * q.groups * q.unit();
-      q = uniform(seq_of<kRows, kWaves>(a, ++seq));
+    while (place - seq_start >= q.places()) {
+      seq_start += q.places();
+      q = uniform(seq_of<kRows, kWaves, kLeast>(a, ++seq));
     }
     const u32 unit = fdy::uniform((place - seq_start) / q.unit()), u_start = seq_start + unit * q.unit(), start = u_start + kEach;
     const u32 next = u_start + q.unit();
@@ -236,8 +725,9 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) tree_kern
     if (q.rounds ? lo >= hi : u_start < share.begin) continue;
     const bool whole = !q.rounds || (lo == start && hi == next);
     const u32 together = q.together, apart = kWaves / together, turn = wave / together;
-    const u32 head = fdy::uniform(unit / q.groups), row0 = unit % q.groups * together * kRows;  // of the workgroup's rows
-    const u32 q0 = row0 + wave % together * kRows;                                         // of the wave's
+    const u32 column0 = unit * together, column = column0 + wave % together;  // the workgroup's first, the wave's
+    const u32 head = column < q.columns ? fdy::uniform(column / q.tiles) : 0, q0 = column < q.columns ? column % q.tiles * kRows : q.rows;
+    const bool works = q0 < q.rows;
     bool bad = q.span.bad;
 
     // the factor of the scores, made positive (its sign goes to the queries)
@@ -248,221 +738,94 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) tree_kern
     Tl::lanes(a, head, z);
 
     x8 qs[kTiles][kSteps];
-    View view[kTiles];
+    u32 draft[kTiles];  // of the lane's rows
 #pragma unroll
     for (int qt = 0; qt < kTiles; ++qt) {
       const u32 r = q0 + qt * 16 + z.col, j = r / a.group, h = r - j * a.group;
-      const bool there = r < q.rows;
+      const bool there = works && r < q.rows;
       const elem* src = (const elem*)a.d.q + (u64)(q.query + j) * a.d.q_token + (u64)(head * a.group + h) * a.d.q_head;
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
-        const u32 e = kF8 ? (st / 2) * 64 + z.grp * 16 + (st & 1) * 8 : st * 32 + z.grp * 8;
+        const u32 e = kF8 && !kShared ? (st / 2) * 64 + z.grp * 16 + (st & 1) * 8 : st * 32 + z.grp * 8;
         v4u32 w = 0;
         if (there && e < D) w = *(const v4u32*)(src + e);
         qs[qt][st] = __builtin_bit_cast(x8, (w & q_keep) ^ q_flip);
       }
-      view[qt] = view_of(a, q, there ? j : 0);
+      draft[qt] = there ? j : 0;
     }
 
-    f32x4 o[kTiles][kParts * kWide];
-    float m[kTiles], sum[kTiles];
-#pragma unroll
-    for (int qt = 0; qt < kTiles; ++qt) {
-      m[qt] = -INFINITY, sum[qt] = 0.f;
-#pragma unroll
-      for (int i = 0; i < kParts * kWide; ++i) o[qt][i] = 0;
-    }
-
+    Sums<T, kDim, kTiles> sums;
+    sums.clear();
     const u32 tile0 = q.span.first / kTile, tiles = q.span.tiles();
     const u32 begin = (lo - start) * apart, end = (hi - start) * apart < tiles ? (hi - start) * apart : tiles;
-    const u32 t_end = fdy::uniform((tile0 + end) * kTile), t_step = apart * kTile;
-    u32 t = fdy::uniform((tile0 + begin + turn) * kTile);
-    // tiles in which rows see different tokens, or tokens are not there
-    const int past = q.base, opens = a.d.window ? (int)(q.span.end - a.d.window) : 0;
-    if (q.rounds && t < t_end && q0 < q.rows) {
-      Tl x;
-      typename Tl::Ids ids = Tl::ids(a, q.span, t, bad);
-      x.load_k(a, z, q.span, ids, t, bad);
-      x.load_v(a, z, q.span, ids, t, bad);
-      for (; t < t_end; t += t_step) {
-        const u32 t_next = t + t_step < t_end ? t + t_step : 0x7fffffc0u;  // behind every row
-        const typename Tl::Ids ids_next = Tl::ids(a, q.span, t_next, bad);
-        f32x4 s[kTiles][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-          for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = 0;
-#pragma unroll
-          for (int st = 0; st < kSteps; ++st) {
-            const x8 key = x.key(u, st);
-#pragma unroll
-            for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = mfma<T>(key, qs[qt][st], s[qt][u]);
-          }
-        }
-        x.load_k(a, z, q.span, ids_next, t_next, bad);
-        const bool mixed = kSmall || (int)(t + kTile) > past || (int)t < opens || (ids.page[0] | ids.page[1]) == ~0u;
-        bool odd = false;
-        u32 shown[kTiles];
-        if (mixed) {
-          u32 there = 0;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) there |= x.seen(a, z, q.span, ids, t, j / 4, j % 4) ? 1u << j : 0;
-#pragma unroll
-          for (int qt = 0; qt < kTiles; ++qt) {
-            const int tok = (int)(t + z.grp * 4);
-            shown[qt] = there & (sees4(a, q, view[qt], tok) | sees4(a, q, view[qt], tok + 16) << 4);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[qt][j / 4][j % 4] = shown[qt] >> j & 1 ? s[qt][j / 4][j % 4] : -INFINITY;
-          }
-          u32 any = 0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int pt = 0; pt < kParts; ++pt)
-#pragma unroll
-              for (int k = 0; k < (int)sizeof(typename Tl::vword) / 4; ++k) any |= odd_mask<T, kF8>(word(x.v[i][pt], k));
-          odd = ballot(any != 0) != 0;
-        }
-        x8 p[kTiles], rest[kTiles];
-        float keep[kTiles], weight[kTiles][8];
-#pragma unroll
-        for (int qt = 0; qt < kTiles; ++qt) {
-          float mx = s[qt][0][0];
-#pragma unroll
-          for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[qt][j / 4][j % 4]);
-          const float m_new = fmaxf(m[qt], over_groups(mx, larger)), ref = m_new == -INFINITY ? 0.f : m_new;
-          keep[qt] = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
-          m[qt] = m_new;
-          float part = 0.f;
-          v4u32 first_of, rest_of;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4] - ref, scale, kLift<T>));
-            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4 + 1] - ref, scale, kLift<T>));
-            part += e0 + e1;
-            weight[qt][2 * j] = e0, weight[qt][2 * j + 1] = e1;
-            u32 hi_of, lo_of;
-            split<T>(e0, e1, hi_of, lo_of);
-            first_of[j] = hi_of, rest_of[j] = lo_of;
-          }
-          p[qt] = __builtin_bit_cast(x8, first_of), rest[qt] = __builtin_bit_cast(x8, rest_of);
-          sum[qt] = sum[qt] * keep[qt] + part;
-        }
-        if (odd) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int pt = 0; pt < kParts; ++pt) {
-              if constexpr (sizeof(typename Tl::vword) == 4) {
-                x.v[i][pt] &= ~odd_mask<T, kF8>(x.v[i][pt]);
-              } else {
-#pragma unroll
-                for (int k = 0; k < (int)sizeof(typename Tl::vword) / 4; ++k) x.v[i][pt][k] &= ~odd_mask<T, kF8>(x.v[i][pt][k]);
-              }
-            }
-        }
-#pragma unroll
-        for (int pt = 0; pt < kParts; ++pt)
-#pragma unroll
-          for (int e2 = 0; e2 < kWide / 2; ++e2) {
-            x8 even, odd_e;
-            x.values(pt, e2, even, odd_e);
-#pragma unroll
-            for (int qt = 0; qt < kTiles; ++qt) {
-              f32x4& c0 = o[qt][pt * kWide + 2 * e2];
-              f32x4& c1 = o[qt][pt * kWide + 2 * e2 + 1];
-              c0 = mfma<T>(even, p[qt], c0 * keep[qt]);
-              c1 = mfma<T>(odd_e, p[qt], c1 * keep[qt]);
-              c0 = mfma<T>(even, rest[qt], c0);
-              c1 = mfma<T>(odd_e, rest[qt], c1);
-            }
-          }
-        if (odd) {  // the elements that were taken out, to the rows that see them
-          for (u32 i = 0; i < kTile; ++i) {
-            const u32 tok = t + i, in_half = i & 15, slot = (i >> 4) * 4 + (in_half & 3), owner = in_half >> 2;
-            if (tok - q.span.first >= q.span.end - q.span.first) continue;
-            const u32 page = (u32)a.d.table[(u64)q.span.row * a.d.row_pages + (tok >> a.page_shift)];
-            if (page >= a.d.kv.n_pages) continue;
-            const uint8_t* from = (const uint8_t*)a.d.kv.v + Tl::place(a, z, page, tok);
-            float w[kTiles];
-#pragma unroll
-            for (int qt = 0; qt < kTiles; ++qt) {
-              float mine = -1.f;  // not seen
-#pragma unroll
-              for (u32 j = 0; j < 8; ++j)
-                if (j == slot && (shown[qt] >> j & 1)) mine = weight[qt][j];
-              w[qt] = __shfl(mine, (int)(z.col + 16 * owner));
-            }
-#pragma unroll
-            for (int pt = 0; pt < kParts; ++pt)
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int e = 0; e < kWide; ++e) {
-                  const u32 d = pt * 16 * kWide + (z.grp * 4 + k) * kWide + e;
-                  if (d >= D) continue;
-                  float y;
-                  if (kF8) {
-                    y = (from[d] & 0x7f) == 0x7f ? NAN : 0.f;
-                  } else {
-                    y = (float)((const elem*)from)[d];
-                  }
-                  if (__builtin_isfinite(y)) continue;
-#pragma unroll
-                  for (int qt = 0; qt < kTiles; ++qt)
-                    if (!(w[qt] < 0.f)) o[qt][pt * kWide + e][k] += w[qt] * y;
-                }
-          }
-        }
-        x.load_v(a, z, q.span, ids_next, t_next, bad);
-        ids = ids_next;
-      }
+    if constexpr (kShared) {
+      if (q.rounds)
+        Way::walk(a, q, head, qs, draft, scale, fdy::uniform(tile0 + begin), fdy::uniform(tile0 + end), apart, turn, works, s_mem, sums, bad);
+    } else {
+      if (q.rounds && works)
+        Way::walk(a, q, z, qs, draft, scale, fdy::uniform((tile0 + begin + turn) * kTile), fdy::uniform((tile0 + end) * kTile),
+                  apart * kTile, sums, bad);
     }
     if (ballot(bad) && lane_id() == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
 
-    // the waves' sums, joined
-#pragma unroll
-    for (int qt = 0; qt < kTiles; ++qt) {
-      sum[qt] = over_groups(sum[qt], plus);
-#pragma unroll
-      for (int pt = 0; pt < kParts; ++pt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < kWide; ++e)
-            s_o[wave][qt * 16 + z.col][pt * 16 * kWide + (z.grp * 4 + i) * kWide + e] = o[qt][pt * kWide + e][i];
-      if (z.grp == 0) s_m[wave][qt * 16 + z.col] = m[qt] * scale - kLift<T>, s_l[wave][qt * 16 + z.col] = sum[qt];
-    }
-    __syncthreads();
     const u32 items = together * kRows * quads;  // item i: four elements of a row
-    auto finish = [&](u32 r, u32 qd, float M, float L, f32x4 y) {
-      const u32 j = (row0 + r) / a.group, h = head * a.group + (row0 + r) - j * a.group;
-      const float v_scale = kF8 && a.d.kv.v_scale ? a.d.kv.v_scale[head] : 1.f;
-      y = y * (L == 0.f ? 0.f : v_scale / L);
-      typedef elem x4 __attribute__((ext_vector_type(4)));
-      *(x4*)((elem*)a.d.out + (u64)(q.query + j) * a.d.out_token + (u64)h * a.d.out_head + qd * 4) = __builtin_convertvector(y, x4);
-      if (qd == 0 && a.d.lse)
-        a.d.lse[(u64)(q.query + j) * a.d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
+    // row r of the workgroup's: its head and its number among the head's rows (~0: none)
+    auto row_of = [&](u32 r, u32& kv_head) {
+      const u32 c = column0 + r / kRows;
+      kv_head = c / q.tiles;
+      const u32 row = (c - kv_head * q.tiles) * kRows + r % kRows;
+      return c < q.columns && row < q.rows ? row : ~0u;
     };
-    for (u32 i = threadIdx.x; i < items; i += kThreads) {
-      const u32 r = i / quads, qd = i - r * quads, c = r / kRows, in = r % kRows;
-      if (row0 + r >= q.rows) continue;
-      float M = -INFINITY;
-      for (u32 w = c; w < kWaves; w += together) M = fmaxf(M, s_m[w][in]);
-      const float ref = M == -INFINITY ? 0.f : M;
-      float L = 0.f;
-      f32x4 y = 0;
-      for (u32 w = c; w < kWaves; w += together) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][in] - ref);
-        L += f * s_l[w][in];
-        y += f * *(const f32x4*)&s_o[w][in][qd * 4];
+    const u32 mine = (share.at * 2 + (start > share.begin)) * part_size;
+    if (kShared && apart == 1) {  // no other wave has sums of these rows
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) {
+        const u32 in = qt * 16 + z.col, r = wave * kRows + in, row = q0 + in;
+        const float L = over_groups(sums.sum[qt], plus), M = sums.m[qt] * scale - kLift<T>;
+        if (!works || row >= q.rows) continue;
+#pragma unroll
+        for (int i = 0; i < kDim / 16; ++i) {
+          const u32 d = Way::element(i, 0, z.grp);
+          if (d >= D) continue;
+          if (whole)
+            finish_row<elem>(a, q, head, row, d, M == -INFINITY ? 0.f : M, L, sums.o[qt][i]);
+          else
+            put_part(parts, mine + r * D + d, sums.o[qt][i]);
+        }
+        if (!whole && z.grp == 0) put_part(parts, mine + kRows * kWaves * D + 2 * r, M, L);
       }
-      if (whole) {
-        finish(r, qd, ref, L, y);
-      } else {
-        const u32 mine = (share.at * 2 + (start > share.begin)) * part_size;
-        put_part(parts, mine + r * D + qd * 4, y);
-        if (qd == 0) put_part(parts, mine + kRows * kWaves * D + 2 * r, M, L);
+    } else {  // the waves' sums, joined
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) {
+        const float sum = over_groups(sums.sum[qt], plus);
+#pragma unroll
+        for (int i = 0; i < kDim / 16; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s_o[wave][qt * 16 + z.col][Way::element(i, k, z.grp)] = sums.o[qt][i][k];
+        if (z.grp == 0) s_m[wave][qt * 16 + z.col] = sums.m[qt] * scale - kLift<T>, s_l[wave][qt * 16 + z.col] = sum;
+      }
+      __syncthreads();
+      for (u32 i = threadIdx.x; i < items; i += kThreads) {
+        const u32 r = i / quads, qd = i - r * quads, c = r / kRows, in = r % kRows;
+        u32 kv_head;
+        const u32 row = row_of(r, kv_head);
+        if (row == ~0u) continue;
+        float M = -INFINITY;
+        for (u32 w = c; w < kWaves; w += together) M = fmaxf(M, s_m[w][in]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float L = 0.f;
+        f32x4 y = 0;
+        for (u32 w = c; w < kWaves; w += together) {
+          const float f = __builtin_amdgcn_exp2f(s_m[w][in] - ref);
+          L += f * s_l[w][in];
+          y += f * *(const f32x4*)&s_o[w][in][qd * 4];
+        }
+        if (whole) {
+          finish_row<elem>(a, q, kv_head, row, qd * 4, ref, L, y);
+        } else {
+          put_part(parts, mine + r * D + qd * 4, y);
+          if (qd == 0) put_part(parts, mine + kRows * kWaves * D + 2 * r, M, L);
+        }
       }
     }
     if (whole) {
@@ -470,48 +833,83 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves)) tree_kern
       continue;
     }
 
-    // the unit's parts, joined by the workgroup that finishes last; its counter is left at zero
-    const u32 first = start / share.per, n_parts = (next - 1) / share.per - first + 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part has arrived where all workgroups see it
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      const u32 before = __hip_atomic_fetch_add(a.counters + first, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      s_last = before == n_parts - 1;
-      if (s_last) __hip_atomic_store(a.counters + first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // where the unit's parts are, written by the workgroup that has the first of them
+    const u32 first = start / share.per;
+    if (first == share.at && threadIdx.x == 0) {
+      Split* split = a.splits + first;
+      split->seq = seq, split->unit = unit, split->second = start > first * share.per;
+      split->parts = (next - 1) / share.per - first + 1;
     }
-    __syncthreads();
-    if (!s_last) continue;  // (s_last is written again only behind the next unit's barriers)
-    const bool second = start > first * share.per;
-    for (u32 i = threadIdx.x; i < items; i += kThreads) {
-      const u32 r = i / quads, qd = i - r * quads;
-      if (row0 + r >= q.rows) continue;
-      float M = -INFINITY, L = 0.f;
-      f32x4 y = 0;
-      for (u32 k0 = 0; k0 < n_parts; k0 += 4) {
-        f32x4 part[4];
-        v2u32 ml[4];
-#pragma unroll
-        for (u32 j = 0; j < 4; ++j) {
-          const u32 k = k0 + j < n_parts ? k0 + j : k0, from = ((first + k) * 2 + (k == 0 && second)) * part_size;
-          part[j] = get_part4(parts, from + r * D + qd * 4);
-          ml[j] = get_part2(parts, from + kRows * kWaves * D + 2 * r);
-        }
-        float top = M;
-#pragma unroll
-        for (u32 j = 0; j < 4; ++j) top = fmaxf(top, as_float(ml[j].x));
-        const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(M - ref);
-        y *= keep, L *= keep, M = top;
-#pragma unroll
-        for (u32 j = 0; j < 4; ++j)
-          if (k0 + j < n_parts) {
-            const float f = __builtin_amdgcn_exp2f(as_float(ml[j].x) - ref);
-            L += f * as_float(ml[j].y);
-            y += f * part[j];
-          }
-      }
-      finish(r, qd, M == -INFINITY ? 0.f : M, L, y);
-    }
+    __syncthreads();  // the next unit's sums go where these lay
   }
+}
+
+// Units in parts, joined: a workgroup for every share that a unit goes on from, and a slice of its rows.  In a launch of its own, which
+// all of the card takes part in (by the workgroup that finished last, through memory: 18 to 30 us for 0.4 MB of parts; so 6 to 9).
+template <typename T, u32 kRows, u32 kWaves, u32 kLeast>
+__global__ void __launch_bounds__(256) tree_join_kernel(Tree a) {
+  typedef typename T::elem elem;
+  const Split* split = a.splits + blockIdx.x;
+  const u32 n_parts = fdy::uniform(split->parts), seq = fdy::uniform(split->seq), unit = fdy::uniform(split->unit);
+  if (n_parts == 0) return;
+  const u32 second = fdy::uniform(split->second), first = blockIdx.x, D = a.d.kv.head_dim, quads = D / 4;
+  const Seq q = uniform(seq_of<kRows, kWaves, kLeast>(a, seq));
+  const u32 part_size = part_floats(kRows * kWaves, D), items = q.together * kRows * quads, column0 = unit * q.together;
+  // kItems items of a thread at once, kAtOnce parts of each
+  auto join = [&](auto n_items, auto at_once) {
+    constexpr u32 kItems = decltype(n_items)::value, kAtOnce = decltype(at_once)::value;
+    const u32 step = gridDim.y * 256;
+    for (u32 i0 = blockIdx.y * 256 + threadIdx.x; i0 < items; i0 += kItems * step) {
+      float M[kItems], L[kItems];
+      f32x4 y[kItems];
+      u32 at[kItems], at_ml[kItems];
+#pragma unroll
+      for (u32 g = 0; g < kItems; ++g) {
+        const u32 i = min(i0 + g * step, items - 1), r = i / quads;
+        at[g] = r * D + (i - r * quads) * 4, at_ml[g] = kRows * kWaves * D + 2 * r;
+        M[g] = -INFINITY, L[g] = 0.f, y[g] = 0;
+      }
+      for (u32 k0 = 0; k0 < n_parts; k0 += kAtOnce) {
+        f32x4 part[kItems][kAtOnce];
+        float m[kItems][kAtOnce], l[kItems][kAtOnce];
+#pragma unroll
+        for (u32 j = 0; j < kAtOnce; ++j) {
+          const u32 k = k0 + j < n_parts ? k0 + j : k0;
+          const float* from = a.parts + (u64)((first + k) * 2 + (k == 0 && second)) * part_size;
+#pragma unroll
+          for (u32 g = 0; g < kItems; ++g) {
+            part[g][j] = *(const f32x4*)(from + at[g]);
+            m[g][j] = from[at_ml[g]], l[g][j] = from[at_ml[g] + 1];
+          }
+        }
+#pragma unroll
+        for (u32 g = 0; g < kItems; ++g) {
+          float top = M[g];
+#pragma unroll
+          for (u32 j = 0; j < kAtOnce; ++j) top = fmaxf(top, m[g][j]);
+          const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(M[g] - ref);
+          y[g] *= keep, L[g] *= keep, M[g] = top;
+#pragma unroll
+          for (u32 j = 0; j < kAtOnce; ++j)
+            if (k0 + j < n_parts) {
+              const float f = __builtin_amdgcn_exp2f(m[g][j] - ref);
+              L[g] += f * l[g][j];
+              y[g] += f * part[g][j];
+            }
+        }
+      }
+#pragma unroll
+      for (u32 g = 0; g < kItems; ++g) {
+        const u32 i = i0 + g * step, r = i / quads, d = (i - r * quads) * 4, c = column0 + r / kRows, head = c / q.tiles;
+        const u32 row = (c - head * q.tiles) * kRows + r % kRows;
+        if (i < items && c < q.columns && row < q.rows) finish_row<elem>(a, q, head, row, d, M[g] == -INFINITY ? 0.f : M[g], L[g], y[g]);
+      }
+    }
+  };
+  if (n_parts <= 4)
+    join(std::integral_constant<u32, 2>(), std::integral_constant<u32, 4>());
+  else
+    join(std::integral_constant<u32, 1>(), std::integral_constant<u32, 8>());
 }
 
 // Workgroups: as many as are resident together, fewer where there are not the rounds.
@@ -520,30 +918,38 @@ u64 most_places(const fdy_draft& d, u32 rows) {
   const u64 tiles = ((u64)d.max_draft * (d.n_q_heads / d.kv.n_heads) + rows - 1) / rows;
   return d.n_seqs * d.kv.n_heads * tiles * (row_tiles(d) + 2 + kEach);
 }
-constexpr u32 kMostShares = kCus * 2;
-constexpr size_t kCounterBytes = kMostShares * 4;
+constexpr u32 kMostShares = kCus * 4;
+constexpr size_t kSplitBytes = kMostShares * sizeof(Split);
 
 template <typename T, bool kF8, int kDim>
 int launch_tree(const Tree& a, hipStream_t stream) {
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
-  auto go = [&](auto kernel, u32 waves) {
-    u64 shares = kCus * resident(kDim, waves);
+  auto go = [&](auto kernel, auto join, u32 rows, u32 waves, u32 of_unit) {
+    u64 shares = kCus * of_unit;
     const u64 most = most_places(a.d, 16) / (kEach + 1) + 1;
     if (shares > most) shares = most;
     hipLaunchKernelGGL(kernel, dim3((u32)shares), dim3(64 * waves), 0, stream, a);
+    const u32 slices = (rows * waves * (a.d.kv.head_dim / 4) + 255) / 256;  // of 256 items of four elements
+    if (shares > 1) hipLaunchKernelGGL(join, dim3((u32)shares, slices < 16 ? slices : 16), dim3(256), 0, stream, a);
   };
   // 32 rows a wave, 16 where their sums would not fit the registers, where pages are small or where there are no more
-  constexpr int kTwo = kDim <= 128 || kF8 ? 2 : 1, kOnce = kNonTemporal;
-  constexpr u32 kMost = kDim <= 128 ? 8 : 4;
+  constexpr int kTwo = kDim <= 128 ? 2 : 1, kOnce = kNonTemporal;
+  constexpr u32 kMost = kDim <= 128 ? 8 : 4, kFew = kDim <= 128 ? 4 : 8;
   const u32 rows = a.d.max_draft * a.group;
+  const bool direct = !kF8 && a.d.kv.head_dim == kDim;
   if (a.d.kv.page_tokens < 16)
-    go(tree_kernel<T, kF8, kDim, true, 0, 1, 4>, 4);
+    go(tree_kernel<T, kF8, kDim, true, 0, 1, 4, false, false>, tree_join_kernel<T, 16, 4, 1>, 16, 4, resident(kDim, 4));
   else if (rows <= 16)
-    go(tree_kernel<T, kF8, kDim, false, kOnce, 1, kMost>, kMost);
+    go(tree_kernel<T, kF8, kDim, false, kOnce, 1, kMost, false, false>, tree_join_kernel<T, 16, kMost, 1>, 16, kMost, resident(kDim, kMost));
   else if (rows <= 16 * kTwo)
-    go(tree_kernel<T, kF8, kDim, false, kOnce, kTwo, kMost>, kMost);
+    go(tree_kernel<T, kF8, kDim, false, kOnce, kTwo, kMost, false, false>, tree_join_kernel<T, 16 * kTwo, kMost, 1>, 16 * kTwo, kMost,
+       resident(kDim, kMost));
+  else if (rows <= 64 && kDim <= 128)
+    go(direct ? tree_kernel<T, kF8, kDim, false, 0, 1, kFew, true, !kF8> : tree_kernel<T, kF8, kDim, false, 0, 1, kFew, true, false>,
+       tree_join_kernel<T, 16, kFew, 4>, 16, kFew, resident(kDim, kFew, true));
   else
-    go(tree_kernel<T, kF8, kDim, false, 0, kTwo, kMost>, kMost);
+    go(direct ? tree_kernel<T, kF8, kDim, false, 0, kTwo, 8, true, !kF8> : tree_kernel<T, kF8, kDim, false, 0, kTwo, 8, true, false>,
+       tree_join_kernel<T, 16 * kTwo, 8, 4>, 16 * kTwo, 8, resident(kDim, 8, true));
   FDY_HIP_TRY(hipGetLastError());
   return FDY_OK;
 }
@@ -571,8 +977,8 @@ bool sizes_valid(const fdy_draft& d) {
 extern "C" size_t fdy_tree_attention_workspace_bytes(const fdy_draft* h) {
   if (!h || !sizes_valid(*h)) return 0;
   // for as many shares and rows as any call has
-  const u32 rows = h->kv.head_dim <= 128 ? 8 * 32 : 4 * 32, shares = kCus;
-  return kCounterBytes + ((size_t)shares * 2 * part_floats(rows, h->kv.head_dim) * 4 + 255) / 256 * 256;
+  const u32 rows = h->kv.head_dim <= 128 ? 8 * 32 : 8 * 16, shares = kCus;  // (twice the shares have half the rows)
+  return kSplitBytes + ((size_t)shares * 2 * part_floats(rows, h->kv.head_dim) * 4 + 255) / 256 * 256;
 }
 
 extern "C" int fdy_tree_attention(const fdy_draft* h, void* d_workspace, size_t workspace_bytes, uint32_t* d_status, void* stream) {
@@ -591,10 +997,11 @@ extern "C" int fdy_tree_attention(const fdy_draft* h, void* d_workspace, size_t 
   a.d = d;
   if (d.window >> 31) a.d.window = 0;  // rows have fewer tokens
   a.status = d_status;
-  a.counters = (u32*)d_workspace;
-  a.parts = (float*)((uint8_t*)d_workspace + kCounterBytes);
+  a.splits = (Split*)d_workspace;
+  a.parts = (float*)((uint8_t*)d_workspace + kSplitBytes);
   a.page_shift = log2_of(d.kv.page_tokens);
   a.group = d.n_q_heads / d.kv.n_heads;
+  a.beside = 1;
   const bool f8 = d.kv.type == FDY_F8;
   if (d.type == FDY_BF16)
     return f8 ? launch_tree<Bf16, true>(a, (hipStream_t)stream) : launch_tree<Bf16, false>(a, (hipStream_t)stream);

@@ -58,7 +58,7 @@ class Drafts:
         desc = self.desc(**kw)
         n = fdd.fdy_tree_attention_workspace_bytes(desc)
         if self.ws is None:
-            self.ws = torch.zeros(n, dtype=torch.uint8, device=DEV)
+            self.ws = torch.randint(0, 256, (n,), dtype=torch.uint8, device=DEV)  # contents are irrelevant
         assert self.ws.numel() >= n
         fdd.fdy_tree_attention(desc, self.ws, n, self.cache.status)
         torch.cuda.synchronize()
@@ -77,7 +77,6 @@ def check(*args, **kw):
     got = p.run()
     assert got[2] == 0
     near(got, p.want(), p.kind)
-    assert bool((p.ws[:2048] == 0).all())  # the counters are left at zero
     return p, got
 
 
@@ -353,7 +352,6 @@ def test_batches_of_many_sizes_in_turn_over_one_workspace():
     for i in [0, 2, 1, 4, 6, 0, 8, 3, 5, 9, 2, 7, 0]:
         problems[i].ws = ws
         near(problems[i].run(), wants[i], "bf16")
-        assert bool((ws[:2048] == 0).all())
 
 
 def test_offsets_behind_32_bits():
