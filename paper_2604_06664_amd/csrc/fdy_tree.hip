@@ -35,14 +35,14 @@ typedef Arg<TreeArg> Tree;
 // columns of a sequence.  `together` waves take as many columns side by side: all of a head, which read the same, and of neighbouring
 // heads where these lie beside each other in a token; the waves that are left over take other tokens: `apart` tiles of 32 a round.
 // A unit is one such group of columns of one sequence; units lie one after the other on a line, kEach places and then a place for
-// every round, and equal shares of the line go to the workgroups.
+// every round, and equal shares of the line go to the workgroups.  Where there is a workgroup for every round, each takes one.
 struct Seq {
   Span span;        // tokens that any of its queries sees
   u32 query, count;  // its first drafted token in q, and how many
   int base;         // tokens ahead of them
   u32 rows, tiles, columns, together, rounds;  // tiles: of a head's rows
-  __device__ u32 unit() const { return rounds + kEach; }
-  __device__ u32 places() const { return (columns + together - 1) / together * unit(); }
+  __device__ u32 units() const { return (columns + together - 1) / together; }
+  __device__ u32 unit(u32 each) const { return rounds + each ? rounds + each : 1; }
 };
 __device__ __forceinline__ Seq uniform(const Seq& v) {
   Seq q;
@@ -89,7 +89,7 @@ __device__ __forceinline__ Seq seq_of(const Tree& a, u32 s) {
 struct TreeShare {
   u32 begin, end, per;  // places
   u32 seq, start;       // the sequence at `begin`, and its own place
-  u32 at;
+  u32 at, each;         // each: places ahead of a unit's rounds
 };
 template <u32 kWaves>
 struct TreeLds {
@@ -102,13 +102,12 @@ __device__ __forceinline__ bool find_tree_share(const Tree& a, TreeShare& out, T
   constexpr u32 kThreads = 64 * kWaves;
   const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + kThreads - 1) / kThreads;
   const u32 s0 = min(tid * slice, n), s1 = min(s0 + slice, n);
-  auto cost = [&](u32 s) {
+  u32 mine = 0;  // places, without any ahead of rounds
+  for (u32 s = s0; s < s1; ++s) {
     const Seq q = seq_of<kRows, kWaves, kLeast>(a, s);
     if (q.span.bad && q.count == 0 && blockIdx.x == 0) raise_status(a.status, FDY_ST_BAD_INDEX);  // no one else looks at it
-    return q.places();
-  };
-  u32 mine = 0;
-  for (u32 s = s0; s < s1; ++s) mine += cost(s);
+    mine += q.units() * q.unit(0);
+  }
   const u32 inc = wave_incl_scan(mine);
   if (lane_id() == 63) lds.sum[tid >> 6] = inc;
   __syncthreads();
@@ -118,20 +117,39 @@ __device__ __forceinline__ bool find_tree_share(const Tree& a, TreeShare& out, T
     if (w < tid >> 6) before += lds.sum[w];
     total += lds.sum[w];
   }
+  out.each = fdy::uniform(total <= gridDim.x ? 0 : kEach);
+  if (out.each) {
+    mine = 0, before = 0, total = 0;
+    for (u32 s = s0; s < s1; ++s) {
+      const Seq q = seq_of<kRows, kWaves, kLeast>(a, s);
+      mine += q.units() * q.unit(kEach);
+    }
+    const u32 inc = wave_incl_scan(mine);
+    __syncthreads();
+    if (lane_id() == 63) lds.sum[tid >> 6] = inc;
+    __syncthreads();
+    before = inc - mine;
+#pragma unroll
+    for (u32 w = 0; w < kWaves; ++w) {
+      if (w < tid >> 6) before += lds.sum[w];
+      total += lds.sum[w];
+    }
+  }
   total = fdy::uniform(total);
   // dies take workgroups in turn: neighbours on the line, which read the same keys and values, go to one
   const u32 g = gridDim.x;
   out.at = g % 8 ? blockIdx.x : blockIdx.x % 8 * (g / 8) + blockIdx.x / 8;
   if (tid == 0) a.splits[out.at].parts = 0;
   if (total == 0) return false;
-  out.per = max((total - 1) / g + 1, kEach + 1);
+  out.per = max((total - 1) / g + 1, out.each + 1);
   if ((u64)out.at * out.per >= total) return false;
   out.begin = out.at * out.per;
   out.end = total - out.begin > out.per ? out.begin + out.per : total;
   if (out.begin >= before && out.begin < before + mine) {
     u32 s = s0;
     for (;; ++s) {
-      const u32 c = cost(s);
+      const Seq q = seq_of<kRows, kWaves, kLeast>(a, s);
+      const u32 c = q.units() * q.unit(out.each);
       if (out.begin < before + c) break;
       before += c;
     }
@@ -422,7 +440,7 @@ struct Together {
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
   static constexpr u32 kEs = kF8 ? 1 : 2, kRow = kDim * 2, kTileBytes = 2 * kTile * kRow;  // of keys, then values
-  static constexpr u32 kMost = kWaves / 4;  // tiles of a stage
+  static constexpr u32 kMost = kDirect && kTiles == 2 ? 4 : kWaves / 4;  // tiles of a stage
   static constexpr u32 kSlot = kMost * kTileBytes;
   static constexpr int kSteps = kDim / 32;
   static constexpr u32 kPieces = 2 * kTile * kDim * kEs / 1024, kMine = (kPieces + kWaves - 1) / kWaves;  // of a tile; of a wave
@@ -714,12 +732,12 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
   u32 seq = share.seq, seq_start = share.start;
   Seq q = uniform(seq_of<kRows, kWaves, kLeast>(a, seq));
   for (u32 place = share.begin; place < share.end;) {
-    while (place - seq_start >= q.places()) {
-      seq_start += q.places();
+    while (place - seq_start >= q.units() * q.unit(share.each)) {
+      seq_start += q.units() * q.unit(share.each);
       q = uniform(seq_of<kRows, kWaves, kLeast>(a, ++seq));
     }
-    const u32 unit = fdy::uniform((place - seq_start) / q.unit()), u_start = seq_start + unit * q.unit(), start = u_start + kEach;
-    const u32 next = u_start + q.unit();
+    const u32 of_unit = q.unit(share.each), unit = fdy::uniform((place - seq_start) / of_unit);
+    const u32 u_start = seq_start + unit * of_unit, start = u_start + share.each, next = u_start + of_unit;
     place = next;
     const u32 lo = start > share.begin ? start : share.begin, hi = next < share.end ? next : share.end;
     if (q.rounds ? lo >= hi : u_start < share.begin) continue;
@@ -810,15 +828,21 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
         u32 kv_head;
         const u32 row = row_of(r, kv_head);
         if (row == ~0u) continue;
-        float M = -INFINITY;
-        for (u32 w = c; w < kWaves; w += together) M = fmaxf(M, s_m[w][in]);
+        constexpr u32 kApart = kWaves / kLeast;  // the most waves that have sums of a row; those behind the last count nothing
+        float m[kApart], l[kApart], M = -INFINITY, L = 0.f;
+        f32x4 o[kApart], y = 0;
+#pragma unroll
+        for (u32 k = 0; k < kApart; ++k) {
+          const u32 w = k < apart ? c + k * together : c;
+          m[k] = k < apart ? s_m[w][in] : -INFINITY, l[k] = s_l[w][in], o[k] = *(const f32x4*)&s_o[w][in][qd * 4];
+        }
+#pragma unroll
+        for (u32 k = 0; k < kApart; ++k) M = fmaxf(M, m[k]);
         const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f;
-        f32x4 y = 0;
-        for (u32 w = c; w < kWaves; w += together) {
-          const float f = __builtin_amdgcn_exp2f(s_m[w][in] - ref);
-          L += f * s_l[w][in];
-          y += f * *(const f32x4*)&s_o[w][in][qd * 4];
+#pragma unroll
+        for (u32 k = 0; k < kApart; ++k) {
+          const float f = __builtin_amdgcn_exp2f(m[k] - ref);
+          if (k < apart) L += f * l[k], y += f * o[k];
         }
         if (whole) {
           finish_row<elem>(a, q, kv_head, row, qd * 4, ref, L, y);
@@ -926,7 +950,7 @@ int launch_tree(const Tree& a, hipStream_t stream) {
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
   auto go = [&](auto kernel, auto join, u32 rows, u32 waves, u32 of_unit) {
     u64 shares = kCus * of_unit;
-    const u64 most = most_places(a.d, 16) / (kEach + 1) + 1;
+    const u64 most = most_places(a.d, 16);
     if (shares > most) shares = most;
     hipLaunchKernelGGL(kernel, dim3((u32)shares), dim3(64 * waves), 0, stream, a);
     const u32 slices = (rows * waves * (a.d.kv.head_dim / 4) + 255) / 256;  // of 256 items of four elements
