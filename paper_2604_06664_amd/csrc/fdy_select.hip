@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(256, kResident<kType>) scores_kernel(Select a)
 }
 
 // ---- choice -----------------------------------------------------------------------------------------
-// One workgroup for a cache head of a sequence: the key that the last one taken has, eight bits at a time from the highest in which
+// One workgroup for a cache head of a sequence: the key that the last one taken has, ten bits at a time from the highest in which
 // the keys differ, then those above it and as many of those equal to it as there is room for, in the order of the row.
 // kMine: keys that a thread holds in registers, every kThreads-th of the row; 0: keys are read again from the workspace, for rows of
 // more pages.
@@ -408,7 +408,8 @@ template <u32 kMine>
 __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
   __shared__ u64 s_low, s_high, s_scan[17];
   __shared__ alignas(16) u32 s_bins[2][kBins];
-  __shared__ u32 s_bin, s_above, s_here, s_ranks[kMine * kWaves + 1];
+  constexpr u32 kRanks = (kMine * kWaves + 63) / 64 * 64;  // a whole number of every lane's, of which those behind the last count nothing
+  __shared__ u32 s_bin, s_above, s_here, s_ranks[kRanks + 1];
   __shared__ u64 s_words[kMine * kWaves + 1];
   const u32 H = a.d.kv.n_heads, s = blockIdx.x / H, g = blockIdx.x % H, tid = threadIdx.x, budget = a.d.budget;
   const u32 wave = tid >> 6, l = lane_id();
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
   };
   auto ranks_ahead = [&] {  // s_ranks, each the sum of those ahead of it
     __syncthreads();
-    constexpr u32 kOf = (kMine * kWaves + 63) / 64;
+    constexpr u32 kOf = kRanks / 64;
     if (wave == 0) {
       u32 c[kOf + 1], sum = 0;
 #pragma unroll
