@@ -549,8 +549,8 @@ __global__ void __launch_bounds__(256) keep_move_kernel(Keep a) {
     return (v4u32*)((uint8_t*)plane + (u32)table[token >> a.shift] * a.d.page_stride + (token & in_page) * a.t.token_stride +
                     piece * a.t.piece_stride + word * 16);
   };
-  if (begin < kept && a.d.n_planes && (u32)keep[begin] >= kept) {
-    const u32 moves = kept - begin;
+  const u32 moves = kept - begin;
+  if (begin < kept && a.d.n_planes && (u32)keep[begin] >= kept && !((u64)moves * words >> 32)) {
     const u64 of_plane = (u64)moves * a.columns;
     const u32 chunks = (u32)((of_plane + kMoved * 256 - 1) / (kMoved * 256));
     for (u64 c = blockIdx.y; c < (u64)chunks * a.d.n_planes; c += gridDim.y) {
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(256) keep_move_kernel(Keep a) {
           const u32 rest = (u32)(at - (u64)token * a.columns);
           piece = rest / words, word = rest - piece * words;
         } else {
-          const u32 of_piece = moves * words;  // below 2^31: `columns` is no less
+          const u32 of_piece = moves * words;
           piece = (u32)(at / of_piece);
           const u32 rest = (u32)(at - (u64)piece * of_piece);
           token = rest / words, word = rest - token * words;
