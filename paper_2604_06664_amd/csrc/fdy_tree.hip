@@ -239,6 +239,29 @@ __device__ __forceinline__ u32 odd_mask(u32 w) {  // all bits of each element of
 }
 
 // ---- a wave's sums ----------------------------------------------------------------------------------
+// Weights are at most 1 with bf16, of whatever size the slack leaves them; f16, which holds them lifted, has no room for any.
+template <typename T>
+inline constexpr float kSlack = kLift<T> == 0.f ? 4.f : 0.f;
+template <typename T>
+inline constexpr float kRaise = kLift<T> - kSlack<T>;
+
+// Weights in two parts, as split(), for those that are worked on beside the matrix cores: bf16 with one operation an element less.  What
+// makes the second part more than nothing is 2^-20 of the weight here.
+template <typename T>
+__device__ __forceinline__ void split_near(float x, float y, u32& first, u32& rest) {
+  split<T>(x, y, first, rest);
+}
+template <>
+__device__ __forceinline__ void split_near<Bf16>(float x, float y, u32& first, u32& rest) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const u32 a = __builtin_bit_cast(u32, x), b = __builtin_bit_cast(u32, y);
+  constexpr float kMore = 1.f + 0x1p-20f;
+  first = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  const bf16x2 r = {(__bf16)__builtin_fmaf(x, kMore, -__builtin_bit_cast(float, a & 0xffff0000u)),
+                    (__bf16)__builtin_fmaf(y, kMore, -__builtin_bit_cast(float, b & 0xffff0000u))};
+  rest = __builtin_bit_cast(u32, r);
+}
+
 template <typename T, int kDim, int kTiles>
 struct Sums {
   typedef typename T::x8 x8;
@@ -254,40 +277,44 @@ struct Sums {
     }
   }
 
-  // The weights of a tile's scores, in two parts; the sums so far are brought to the new maximum.
-  __device__ __forceinline__ void weigh(const f32x4 (*s)[2], float scale, x8* p, x8* rest) {
-    float keep[kTiles];
+  // The weights of a tile's scores, in two parts: 2^kRaise e^(x - m).  m follows the maximum once that is more than 2^kSlack ahead of it:
+  // in the first few tiles and then hardly ever, where the maximum of one of 32 rows moves in three tiles of five.
+  __device__ __forceinline__ void follow(const f32x4 (*s)[2], float scale) {
+    float top[kTiles];
+    bool moved = false;
 #pragma unroll
     for (int qt = 0; qt < kTiles; ++qt) {
       float mx = s[qt][0][0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) mx = fmaxf(mx, s[qt][j / 4][j % 4]);
-      const float m_new = fmaxf(m[qt], over_groups(mx, larger)), ref = m_new == -INFINITY ? 0.f : m_new;
-      keep[qt] = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
-      m[qt] = m_new;
-      float part = 0.f;
-      v4u32 first_of, rest_of;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4] - ref, scale, kLift<T>));
-        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4 + 1] - ref, scale, kLift<T>));
-        part += e0 + e1;
-        u32 hi_of, lo_of;
-        split<T>(e0, e1, hi_of, lo_of);
-        first_of[j] = hi_of, rest_of[j] = lo_of;
-      }
-      p[qt] = __builtin_bit_cast(x8, first_of), rest[qt] = __builtin_bit_cast(x8, rest_of);
-      sum[qt] = sum[qt] * keep[qt] + part;
+      top[qt] = over_groups(mx, larger);
+      moved |= (top[qt] - m[qt]) * scale > kSlack<T>;
     }
-    // (the maximum moves seldom once some tiles have been seen)
-    bool moved = false;
-#pragma unroll
-    for (int qt = 0; qt < kTiles; ++qt) moved |= keep[qt] != 1.f;
     if (ballot(moved))
 #pragma unroll
-      for (int qt = 0; qt < kTiles; ++qt)
+      for (int qt = 0; qt < kTiles; ++qt) {
+        const float m_new = (top[qt] - m[qt]) * scale > kSlack<T> ? top[qt] : m[qt], ref = m_new == -INFINITY ? 0.f : m_new;
+        const float keep = __builtin_amdgcn_exp2f((m[qt] - ref) * scale);
+        m[qt] = m_new, sum[qt] *= keep;
 #pragma unroll
-        for (int i = 0; i < kDim / 16; ++i) o[qt][i] *= keep[qt];
+        for (int i = 0; i < kDim / 16; ++i) o[qt][i] *= keep;
+      }
+  }
+  // Two of a row's weights, and all of them.
+  __device__ __forceinline__ void weigh2(const f32x4 (*s)[2], float scale, int qt, int j, v4u32* first_of, v4u32* rest_of) {
+    const float ref = m[qt] == -INFINITY ? 0.f : m[qt];
+    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4] - ref, scale, kRaise<T>));
+    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 2][2 * j % 4 + 1] - ref, scale, kRaise<T>));
+    sum[qt] += e0 + e1;
+    u32 hi_of, lo_of;
+    split_near<T>(e0, e1, hi_of, lo_of);
+    first_of[qt][j] = hi_of, rest_of[qt][j] = lo_of;
+  }
+  __device__ __forceinline__ void weigh(const f32x4 (*s)[2], float scale, v4u32* first_of, v4u32* rest_of) {
+#pragma unroll
+    for (int qt = 0; qt < kTiles; ++qt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) weigh2(s, scale, qt, j, first_of, rest_of);
   }
 };
 
@@ -296,7 +323,9 @@ template <int kTiles>
 __device__ __forceinline__ void show(const Tree& a, const Seq& q, const u32* draft, u32 there, int tok, f32x4 (*s)[2]) {
 #pragma unroll
   for (int qt = 0; qt < kTiles; ++qt) {
-    const View view = view_of(a, q, draft[qt]);
+    u32 j0 = draft[qt];
+    asm volatile("" : "+v"(j0));  // (nothing of this is worked out ahead of the loop over tiles, where registers are short)
+    const View view = view_of(a, q, j0);
     const u32 shown = there & (sees4(a, q, view, tok) | sees4(a, q, view, tok + 16) << 4);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[qt][j / 4][j % 4] = shown >> j & 1 ? s[qt][j / 4][j % 4] : -INFINITY;
@@ -375,7 +404,8 @@ struct Alone {
             }
         odd = ballot(any != 0) != 0;
       }
-      x8 p[kTiles], rest[kTiles];
+      v4u32 p[kTiles], rest[kTiles];
+      sums.follow(s, scale);
       sums.weigh(s, scale, p, rest);
 #pragma unroll
       for (int pt = 0; pt < kParts; ++pt)
@@ -387,10 +417,10 @@ struct Alone {
           for (int qt = 0; qt < kTiles; ++qt) {
             f32x4& c0 = sums.o[qt][pt * kWide + 2 * e2];
             f32x4& c1 = sums.o[qt][pt * kWide + 2 * e2 + 1];
-            c0 = mfma<T>(even, p[qt], c0);
-            c1 = mfma<T>(odd_e, p[qt], c1);
-            c0 = mfma<T>(even, rest[qt], c0);
-            c1 = mfma<T>(odd_e, rest[qt], c1);
+            c0 = mfma<T>(even, __builtin_bit_cast(x8, p[qt]), c0);
+            c1 = mfma<T>(odd_e, __builtin_bit_cast(x8, p[qt]), c1);
+            c0 = mfma<T>(even, __builtin_bit_cast(x8, rest[qt]), c0);
+            c1 = mfma<T>(odd_e, __builtin_bit_cast(x8, rest[qt]), c1);
           }
         }
       if (odd) {  // the elements that were taken out, to the rows that see them: whatever the weight is, it is not 0
@@ -560,29 +590,45 @@ struct Together {
     return __builtin_bit_cast(x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 
-  // A tile that lies at `k`.  kPlain: all its rows see all of its tokens.
-  template <bool kPlain>
-  static __device__ __forceinline__ void take(const Tree& a, const Seq& q, const uint8_t* k, u32 t, u32 pages, const x8 (*qs)[kSteps],
-                                              const u32* draft, float scale, Sums<T, kDim, kTiles>& sums) {
+  // The scores of a tile whose keys lie at `k`; c of 2 kSteps is a step and a half of the tile.
+  static __device__ __forceinline__ u32 key_at() {
     const u32 l = lane_id(), col = l & 15, grp = l >> 4;
-    const uint8_t* v = k + kTile * kRow;
-    u32 k_at = col * kRow + ((grp >> 1 ^ turn(col)) * 32 + (grp & 1) * 16);
+    u32 at = col * kRow + ((grp >> 1 ^ turn(col)) * 32 + (grp & 1) * 16);
+    asm volatile("" : "+v"(at));  // worked out again for each tile: what follows from it would take half a dozen registers
+    return at;
+  }
+  static __device__ __forceinline__ x8 key(const uint8_t* k, u32 at, int c) {
+    return __builtin_bit_cast(x8, *(const v4u32*)(k + (at ^ c / 2 * 64) + c % 2 * 16 * kRow));
+  }
+  static __device__ __forceinline__ void score(const uint8_t* k, const x8 (*qs)[kSteps], f32x4 (*s)[2]) {
+    const u32 at = key_at();
+#pragma unroll
+    for (int c = 0; c < 2 * kSteps; ++c) {
+      const x8 x = key(k, at, c);
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) s[qt][c % 2] = mfma<T>(x, qs[qt][c / 2], c < 2 ? (f32x4)(0.f) : s[qt][c % 2]);
+    }
+  }
+
+  // A tile whose values lie at `v`, with the scores s.  kPlain: all its rows see all of its tokens.  kOn: the scores of the tile at
+  // k_next replace s; the matrix cores work on them while the vector unit does on this tile's weights.  With two waves a SIMD
+  // little else hides how long LDS takes to answer, so the order of reads is the one written here: the first values ahead of the weights.
+  template <bool kPlain, bool kOn>
+  static __device__ __forceinline__ void take(const Tree& a, const Seq& q, const uint8_t* v, const uint8_t* k_next, u32 t, u32 pages,
+                                              const x8 (*qs)[kSteps], const u32* draft, float scale, f32x4 (*s)[2],
+                                              Sums<T, kDim, kTiles>& sums) {
+    constexpr int kValues = kDim / 16, kAhead = 4;
+    u32 l = lane_id();
+    if (!kPlain) asm volatile("" : "+v"(l));  // as in show()
+    const u32 col = l & 15, grp = l >> 4;
     const u32 v_token = grp * 4 + (col >> 2);
     u32 v_at = v_token * kRow + (turn(v_token) * 32 + (col & 3) * 8);
-    asm volatile("" : "+v"(k_at), "+v"(v_at));  // worked out again for each tile: what follows from them would take a dozen registers
-    f32x4 s[kTiles][2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = 0;
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const x8 key = __builtin_bit_cast(x8, *(const v4u32*)(k + (k_at ^ st * 64) + u * 16 * kRow));
-#pragma unroll
-        for (int qt = 0; qt < kTiles; ++qt) s[qt][u] = mfma<T>(key, qs[qt][st], s[qt][u]);
-      }
+    asm volatile("" : "+v"(v_at));
+    x8 values[kValues];
+    constexpr int kTurns = 2 * kSteps, kPairs = 4 * kTiles;
+    x8 x0, x1;
+    u32 at = 0;
+    if constexpr (kOn) at = key_at(), x0 = key(k_next, at, 0), x1 = key(k_next, at, 1);
     u32 there = 0, any = 0;
     if (!kPlain) {
 #pragma unroll
@@ -592,11 +638,33 @@ struct Together {
       }
       show<kTiles>(a, q, draft, there, (int)(t + grp * 4), s);
     }
-    x8 p[kTiles], rest[kTiles];
-    sums.weigh(s, scale, p, rest);
+    v4u32 p[kTiles], rest[kTiles];
+    sums.follow(s, scale);
+    f32x4 s_next[kTiles][2];
+    if constexpr (kOn) {
 #pragma unroll
-    for (int i = 0; i < kDim / 16; ++i) {
-      x8 x = value(v, v_at, i);
+      for (int c = 0; c < kTurns; ++c) {
+        const x8 x2 = c + 2 < kTurns ? key(k_next, at, c + 2) : x0;
+        if (c + kAhead >= kTurns) values[c + kAhead - kTurns] = value(v, v_at, c + kAhead - kTurns);
+#pragma unroll
+        for (int qt = 0; qt < kTiles; ++qt) s_next[qt][c % 2] = mfma<T>(x0, qs[qt][c / 2], c < 2 ? (f32x4)(0.f) : s_next[qt][c % 2]);
+#pragma unroll
+        for (int i = c * kPairs / kTurns; i < (c + 1) * kPairs / kTurns; ++i) sums.weigh2(s, scale, i / 4, i % 4, p, rest);
+        __builtin_amdgcn_sched_barrier(0);
+        x0 = x1, x1 = x2;
+      }
+#pragma unroll
+      for (int qt = 0; qt < kTiles; ++qt) s[qt][0] = s_next[qt][0], s[qt][1] = s_next[qt][1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) values[i] = value(v, v_at, i);
+      sums.weigh(s, scale, p, rest);
+    }
+    __builtin_amdgcn_s_setprio(1);  // products ahead of another wave's weights: 275 us -> 271 (eight wide trees)
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      if (i + kAhead < kValues) values[i + kAhead] = value(v, v_at, i + kAhead);
+      x8 x = values[i];
       if (!kPlain) {  // nothing of tokens that are not there, and no infinities
         v4u32 y = __builtin_bit_cast(v4u32, x);
 #pragma unroll
@@ -609,18 +677,25 @@ struct Together {
         x = __builtin_bit_cast(x8, y);
       }
 #pragma unroll
-      for (int qt = 0; qt < kTiles; ++qt) sums.o[qt][i] = mfma<T>(x, p[qt], sums.o[qt][i]);
+      for (int qt = 0; qt < kTiles; ++qt) sums.o[qt][i] = mfma<T>(x, __builtin_bit_cast(x8, p[qt]), sums.o[qt][i]);
 #pragma unroll
-      for (int qt = 0; qt < kTiles; ++qt) sums.o[qt][i] = mfma<T>(x, rest[qt], sums.o[qt][i]);
+      for (int qt = 0; qt < kTiles; ++qt) sums.o[qt][i] = mfma<T>(x, __builtin_bit_cast(x8, rest[qt]), sums.o[qt][i]);
+      if (kOn) __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     if (!kPlain && ballot(any != 0)) {  // what was taken out, to the rows that see it: whatever the weight is, it is not 0
       u32 seen[kTiles];
 #pragma unroll
-      for (int qt = 0; qt < kTiles; ++qt) seen[qt] = tokens_seen(a, q, view_of(a, q, draft[qt]), there, (int)(t + grp * 4));
+      for (int qt = 0; qt < kTiles; ++qt) {
+        u32 j0 = draft[qt];
+        asm volatile("" : "+v"(j0));
+        seen[qt] = tokens_seen(a, q, view_of(a, q, j0), there, (int)(t + grp * 4));
+      }
       for (u32 token = 0; token < kTile; ++token) {
         if (t + token - q.span.first >= q.span.end - q.span.first || !(pages >> token / 16 & 1)) continue;
 #pragma unroll
-        for (int i = 0; i < kDim / 16; ++i)
+        for (int i = 0; i < kDim / 16; ++i) {
+          asm volatile("" ::: "memory");  // a few at a time: this is seldom
 #pragma unroll
           for (u32 e = 0; e < 4; ++e) {
             const float y = (float)*(const elem*)(v + token * kRow + ((i ^ turn(token)) * 32 + (grp * 4 + e) * 2));
@@ -629,6 +704,7 @@ struct Together {
             for (int qt = 0; qt < kTiles; ++qt)
               if (seen[qt] >> token & 1) sums.o[qt][i][e] += y;
           }
+        }
       }
     }
   }
@@ -675,15 +751,23 @@ struct Together {
         look_up(a, q, tile + 3 * step, ids, bad);
       }
       const u32 n = count(tile);
-      if (works)
-        for (u32 i = mine; i < n; i += apart) {
-          const u32 t = (tile + i) * kTile, of = pages >> 2 * i & 3;
-          const uint8_t* k = lds + slot * kSlot + i * kTileBytes;
-          if (of == 3 && (int)(t + kTile) <= q.base && (int)t >= opens)
-            take<true>(a, q, k, t, of, qs, draft, scale, sums);
-          else
-            take<false>(a, q, k, t, of, qs, draft, scale, sums);
+      if (works && mine < n) {
+        const uint8_t* k = lds + slot * kSlot + mine * kTileBytes;
+        f32x4 s[kTiles][2];
+        const u32 first = tile * kTile;
+        if ((~pages & ((1u << 2 * n) - 1)) == 0 && (int)(first + n * kTile) <= q.base && (int)first >= opens) {
+          score(k, qs, s);
+          u32 i = mine;
+          for (; i + apart < n; i += apart, k += apart * kTileBytes)
+            take<true, true>(a, q, k + kTile * kRow, k + apart * kTileBytes, 0, 3, qs, draft, scale, s, sums);
+          take<true, false>(a, q, k + kTile * kRow, k, 0, 3, qs, draft, scale, s, sums);
+        } else {
+          for (u32 i = mine; i < n; i += apart, k += apart * kTileBytes) {
+            score(k, qs, s);
+            take<false, false>(a, q, k + kTile * kRow, k, (tile + i) * kTile, pages >> 2 * i & 3, qs, draft, scale, s, sums);
+          }
         }
+      }
       pages = pages_next, pages_next = pages_then;
     }
     __syncthreads();  // what follows goes where the slots lie
@@ -786,6 +870,8 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
     }
     if (ballot(bad) && lane_id() == 0) raise_status(a.status, FDY_ST_BAD_INDEX);
 
+    u32 tid = threadIdx.x;
+    asm volatile("" : "+v"(z.col), "+v"(z.grp), "+v"(tid));  // nothing of what follows is worked out ahead of the tiles
     const u32 items = together * kRows * quads;  // item i: four elements of a row
     // row r of the workgroup's: its head and its number among the head's rows (~0: none)
     auto row_of = [&](u32 r, u32& kv_head) {
@@ -799,7 +885,7 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
 #pragma unroll
       for (int qt = 0; qt < kTiles; ++qt) {
         const u32 in = qt * 16 + z.col, r = wave * kRows + in, row = q0 + in;
-        const float L = over_groups(sums.sum[qt], plus), M = sums.m[qt] * scale - kLift<T>;
+        const float L = over_groups(sums.sum[qt], plus), M = sums.m[qt] * scale - kRaise<T>;
         if (!works || row >= q.rows) continue;
 #pragma unroll
         for (int i = 0; i < kDim / 16; ++i) {
@@ -820,10 +906,10 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
         for (int i = 0; i < kDim / 16; ++i)
 #pragma unroll
           for (int k = 0; k < 4; ++k) s_o[wave][qt * 16 + z.col][Way::element(i, k, z.grp)] = sums.o[qt][i][k];
-        if (z.grp == 0) s_m[wave][qt * 16 + z.col] = sums.m[qt] * scale - kLift<T>, s_l[wave][qt * 16 + z.col] = sum;
+        if (z.grp == 0) s_m[wave][qt * 16 + z.col] = sums.m[qt] * scale - kRaise<T>, s_l[wave][qt * 16 + z.col] = sum;
       }
       __syncthreads();
-      for (u32 i = threadIdx.x; i < items; i += kThreads) {
+      for (u32 i = tid; i < items; i += kThreads) {
         const u32 r = i / quads, qd = i - r * quads, c = r / kRows, in = r % kRows;
         u32 kv_head;
         const u32 row = row_of(r, kv_head);
