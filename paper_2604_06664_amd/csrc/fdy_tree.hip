@@ -464,8 +464,10 @@ struct Alone {
 // 16 tokens) nor the values' columns (16 elements of 4 tokens, which the transposing read hands out token by token) meet in a bank.
 // o[.][i][k] is of element 16 i + 4 grp + k.
 //
-// kDirect: straight from the pages to LDS, which 16-bit elements and heads of exactly kDim allow.
-template <typename T, bool kF8, int kDim, int kTiles, bool kDirect, u32 kWaves>
+// kDirect: straight from the pages to LDS, which 16-bit elements and heads of exactly kDim allow.  kSmall: pages of less than 16 tokens;
+// a wave looks up the page of every token of a stage, a lane each, and hands them to the lanes that read (248 rows a head over pages of 8
+// tokens, 16 rows of 5,319: 433 us where every 16 rows read for themselves, 147 so).
+template <typename T, bool kF8, int kDim, int kTiles, bool kDirect, u32 kWaves, bool kSmall>
 struct Together {
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
@@ -480,14 +482,29 @@ struct Together {
 
   // Pages of a stage's tiles (0 where a number is none: what comes of it is not looked at).  Tiles that reach over the row's ends take
   // its first or last page there.
+  typedef typename std::conditional<kSmall, u64, u32>::type Bits;  // of halves of tiles that have a page, or of tokens
+  static_assert(!kSmall || (!kDirect && kMost <= 2), "a lane for every token of a stage");
   struct Ids {
-    u32 page[kMost][2], there;  // there: bits 2 i + u of the halves that have a page
+    u32 page[kMost][2];
+    Bits there;
   };
+  static __device__ __forceinline__ Bits of_tile(Bits pages, u32 i) { return kSmall ? pages >> 32 * i & 0xffffffffu : pages >> 2 * i & 3; }
+  static __device__ __forceinline__ bool has_page(Bits of, u32 token) { return of >> (kSmall ? token : token / 16) & 1; }
+  static __device__ __forceinline__ bool all_there(Bits pages, u32 n) { return !(~pages & (((Bits)1 << (kSmall ? 16 : 1) * n << (kSmall ? 16 : 1) * n) - 1)); }
   static __device__ __forceinline__ void look_up(const Tree& a, const Seq& q, u32 tile, Ids& ids, bool& bad) {
     typedef const __attribute__((address_space(4))) u32* table_t;  // no one writes it while the kernel runs
     const table_t table = (table_t)(uintptr_t)(a.d.table + (u64)q.span.row * a.d.row_pages);
     const u32 low = q.span.first >> a.page_shift, high = (q.span.end - 1) >> a.page_shift;
     ids.there = 0;
+    if constexpr (kSmall) {
+      const u32 l = lane_id(), j = (tile * kTile + (kMost > 1 ? l : l % kTile)) >> a.page_shift;
+      const u32 page = (u32)a.d.table[(u64)q.span.row * a.d.row_pages + max(low, min(j, high))];
+      const bool ok = page < a.d.kv.n_pages;
+      ids.there = ballot(ok);
+      ids.page[0][0] = ok ? page : 0;
+      bad |= !ok;
+      return;
+    }
 #pragma unroll
     for (u32 i = 0; i < kMost; ++i)
 #pragma unroll
@@ -500,7 +517,7 @@ struct Together {
 #pragma unroll
       for (u32 u = 0; u < 2; ++u) {
         const bool ok = ids.page[i][u] < a.d.kv.n_pages;
-        ids.there |= ok ? 1u << (2 * i + u) : 0;
+        ids.there |= ok ? (Bits)1 << (2 * i + u) : 0;
         ids.page[i][u] = ok ? ids.page[i][u] : 0;
         bad |= !ok;
       }
@@ -515,13 +532,27 @@ struct Together {
       const u32 token = token_of(wave + m * kWaves) + in;
       // 16-bit: the lane's 16 bytes go to half c % 2 of chunk c / 2; 8-bit: they are a chunk
       const u32 chunk = (kF8 ? c : c / 2) ^ turn(token), at = kF8 ? chunk * 16 : chunk * 32 + c % 2 * 16;
-      lane_at[m] = at < a.d.kv.head_dim * kEs ? (token & 15) * token_bytes + at : kNowhere;
+      lane_at[m] = at < a.d.kv.head_dim * kEs ? (kSmall ? 0 : (token & 15) * token_bytes) + at : kNowhere;
     }
   }
   static __device__ __forceinline__ u32 token_of(u32 piece) { return piece % (kPieces / 2) * kTokens; }
   __device__ __forceinline__ void load(const Tree& a, u32 of_head, u32 wave, u32 tile, u32 n, const Ids& ids) {
     const u64 page_bytes = a.d.kv.page_stride * kEs;
     const u32 token_bytes = (u32)a.d.kv.token_stride * kEs;
+    if constexpr (kSmall) {
+#pragma unroll
+      for (u32 i = 0; i < kMost; ++i)
+#pragma unroll
+        for (u32 m = 0; m < kMine; ++m) {
+          const u32 piece = wave + m * kWaves, token = i * kTile + token_of(piece) + lane_id() / kLanes;
+          const u32 page = (u32)__shfl((int)ids.page[0][0], (int)token);
+          w[i][m] = 0;
+          if (i < n && piece < kPieces && lane_at[m] != kNowhere)
+            w[i][m] = *(const v4u32*)((const uint8_t*)(piece >= kPieces / 2 ? a.d.kv.v : a.d.kv.k) + page * page_bytes +
+                                      ((tile * kTile + token) & (a.d.kv.page_tokens - 1)) * (u64)token_bytes + of_head + lane_at[m]);
+        }
+      return;
+    }
 #pragma unroll
     for (u32 i = 0; i < kMost; ++i)
 #pragma unroll
@@ -614,7 +645,7 @@ struct Together {
   // k_next replace s; the matrix cores work on them while the vector unit does on this tile's weights.  With two waves a SIMD
   // little else hides how long LDS takes to answer, so the order of reads is the one written here: the first values ahead of the weights.
   template <bool kPlain, bool kOn>
-  static __device__ __forceinline__ void take(const Tree& a, const Seq& q, const uint8_t* v, const uint8_t* k_next, u32 t, u32 pages,
+  static __device__ __forceinline__ void take(const Tree& a, const Seq& q, const uint8_t* v, const uint8_t* k_next, u32 t, Bits pages,
                                               const x8 (*qs)[kSteps], const u32* draft, float scale, f32x4 (*s)[2],
                                               Sums<T, kDim, kTiles>& sums) {
     constexpr int kValues = kDim / 16, kAhead = 4;
@@ -634,7 +665,7 @@ struct Together {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const u32 tok = t + (j / 4) * 16 + grp * 4 + j % 4;
-        if (tok - q.span.first < q.span.end - q.span.first && (pages >> (j / 4) & 1)) there |= 1u << j;
+        if (tok - q.span.first < q.span.end - q.span.first && has_page(pages, tok - t)) there |= 1u << j;
       }
       show<kTiles>(a, q, draft, there, (int)(t + grp * 4), s);
     }
@@ -692,7 +723,7 @@ struct Together {
         seen[qt] = tokens_seen(a, q, view_of(a, q, j0), there, (int)(t + grp * 4));
       }
       for (u32 token = 0; token < kTile; ++token) {
-        if (t + token - q.span.first >= q.span.end - q.span.first || !(pages >> token / 16 & 1)) continue;
+        if (t + token - q.span.first >= q.span.end - q.span.first || !has_page(pages, token)) continue;
 #pragma unroll
         for (int i = 0; i < kDim / 16; ++i) {
           asm volatile("" ::: "memory");  // a few at a time: this is seldom
@@ -727,7 +758,8 @@ struct Together {
       x.bring(a, of_head, wave, tile, count(tile), ids, at);
     else
       x.load(a, of_head, wave, tile, count(tile), ids);
-    u32 pages = ids.there, pages_next = 0, slot = 0;
+    u32 slot = 0;
+    Bits pages = ids.there, pages_next = 0;
     look_up(a, q, tile + step, ids, bad);
     if (!kDirect) {
       x.store(lds, wave, count(tile));
@@ -739,7 +771,7 @@ struct Together {
     for (; tile < end; tile += step, slot ^= 1) {
       if (kDirect) arrived();
       __syncthreads();  // the slot is filled, the other one read
-      u32 pages_then = 0;
+      Bits pages_then = 0;
       if (kDirect) {
         x.bring(a, of_head, wave, tile + step, count(tile + step), ids, at + (slot ^ 1) * kSlot);
         pages_next = ids.there;
@@ -755,7 +787,7 @@ struct Together {
         const uint8_t* k = lds + slot * kSlot + mine * kTileBytes;
         f32x4 s[kTiles][2];
         const u32 first = tile * kTile;
-        if ((~pages & ((1u << 2 * n) - 1)) == 0 && (int)(first + n * kTile) <= q.base && (int)first >= opens) {
+        if (all_there(pages, n) && (int)(first + n * kTile) <= q.base && (int)first >= opens) {
           score(k, qs, s);
           u32 i = mine;
           for (; i + apart < n; i += apart, k += apart * kTileBytes)
@@ -764,7 +796,7 @@ struct Together {
         } else {
           for (u32 i = mine; i < n; i += apart, k += apart * kTileBytes) {
             score(k, qs, s);
-            take<false, false>(a, q, k + kTile * kRow, k, (tile + i) * kTile, pages >> 2 * i & 3, qs, draft, scale, s, sums);
+            take<false, false>(a, q, k + kTile * kRow, k, (tile + i) * kTile, of_tile(pages, i), qs, draft, scale, s, sums);
           }
         }
       }
@@ -793,7 +825,7 @@ constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves
 template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves, bool kShared, bool kDirect>
 __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) * kWaves / 4) tree_kernel(Tree a) {
   typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
-  typedef Together<T, kF8, kDim, kTiles, kDirect, kWaves> Both;
+  typedef Together<T, kF8, kDim, kTiles, kDirect, kWaves, kSmall && kShared> Both;
   typedef typename std::conditional<kShared, Both, Alone<T, kF8, kDim, kSmall, kPolicy, kTiles>>::type Way;
   typedef typename T::x8 x8;
   typedef typename T::elem elem;
@@ -1042,13 +1074,18 @@ int launch_tree(const Tree& a, hipStream_t stream) {
     const u32 slices = (rows * waves * (a.d.kv.head_dim / 4) + 255) / 256;  // of 256 items of four elements
     if (shares > 1) hipLaunchKernelGGL(join, dim3((u32)shares, slices < 16 ? slices : 16), dim3(256), 0, stream, a);
   };
-  // 32 rows a wave, 16 where their sums would not fit the registers, where pages are small or where there are no more
+  // 32 rows a wave, 16 where their sums would not fit the registers or where there are no more
   constexpr int kTwo = kDim <= 128 ? 2 : 1, kOnce = kNonTemporal;
   constexpr u32 kMost = kDim <= 128 ? 8 : 4, kFew = kDim <= 128 ? 4 : 8;
   const u32 rows = a.d.max_draft * a.group;
   const bool direct = !kF8 && a.d.kv.head_dim == kDim;
-  if (a.d.kv.page_tokens < 16)
+  const bool small = a.d.kv.page_tokens < 16;
+  if (small && rows <= 16)
     go(tree_kernel<T, kF8, kDim, true, 0, 1, 4, false, false>, tree_join_kernel<T, 16, 4, 1>, 16, 4, resident(kDim, 4));
+  else if (small && rows <= 64 && kDim <= 128)
+    go(tree_kernel<T, kF8, kDim, true, 0, 1, kFew, true, false>, tree_join_kernel<T, 16, kFew, 4>, 16, kFew, resident(kDim, kFew, true));
+  else if (small)
+    go(tree_kernel<T, kF8, kDim, true, 0, kTwo, 8, true, false>, tree_join_kernel<T, 16 * kTwo, 8, 4>, 16 * kTwo, 8, resident(kDim, 8, true));
   else if (rows <= 16)
     go(tree_kernel<T, kF8, kDim, false, kOnce, 1, kMost, false, false>, tree_join_kernel<T, 16, kMost, 1>, 16, kMost, resident(kDim, kMost));
   else if (rows <= 16 * kTwo)

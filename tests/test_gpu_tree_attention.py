@@ -396,3 +396,63 @@ def test_replays_while_rows_and_trees_change():
         assert bool((p.out[T:] == 5).all())
         near((p.run()[0][:T], p.lse[:T].cpu()), p.want(q=p.q[:T]), "bf16")  # eager work between the replays
     assert int(p.cache.status) == 0
+
+
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f8")])
+@pytest.mark.parametrize("D", [48, 64, 128, 192])
+@pytest.mark.parametrize("pt", [1, 8])
+def test_many_rows_over_small_pages(pt, D, kind, cache):
+    """20 to 280 query rows of a cache head, over pages of fewer tokens than a tile's half, in parts and with a window."""
+    check([300, 77, 70], [5, 2, 3], 4, 1, D, kind=kind, cache=cache, pt=pt)
+    check([700, 333], [70, 40], 4, 1, D, kind=kind, cache=cache, pt=pt, order="head")
+    check([400, 90], [12, 40], 4, 1, D, kind=kind, cache=cache, pt=pt, window=100, shape="chain")
+
+
+@pytest.mark.parametrize("drafts", [[12, 3], [40, 9]])
+@pytest.mark.parametrize("pt,cache", [(16, "bf16"), (16, "f8"), (4, "bf16"), (4, "f8")])
+def test_pages_that_are_none_under_many_rows(pt, cache, drafts):
+    p = Drafts([300, 140], drafts, 4, 1, 64, cache=cache, pt=pt, seed=3)
+    c = p.cache
+    table = c.table.copy()
+    table[0, 0], table[0, 96 // pt], table[1, 139 // pt] = -1, c.n_pages, 1 << 30  # the first, one inside a plain tile, the last
+    c.d_table.copy_(torch.from_numpy(table))
+    got = p.run()
+    assert got[2] == od.ST_BAD_INDEX
+    near(got, p.want(table=table), "bf16")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("drafts", [[2, 1], [40, 9]])
+def test_scores_that_grow_along_the_row(drafts, kind):
+    """Every tile's scores are larger than all before by half a power of two to several: the sums are brought to a new maximum, or not yet."""
+    for step in (0.05, 0.3, 1.0):
+        p = Drafts([400, 260], drafts, 4, 2, 64, kind=kind, scale=1.0, shape="chain")
+        c = p.cache
+        p.q[:] = 0
+        p.q[:, :, 0] = 1
+        p.d_q.copy_(p.q)
+        for r, n in enumerate(c.lens):
+            for t in range(n):
+                c.views[0][c.table[r, t // 16], t % 16] = 0
+                c.views[0][c.table[r, t // 16], t % 16, :, 0] = step * (t // 8)
+        c.upload()
+        got = p.run()
+        assert got[2] == 0
+        near(got, p.want(), kind)  # (one product a score, of at most 50: exact but for the factor's 2^-23 of it)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("drafts", [[2, 1], [40, 9]])
+def test_values_near_the_end_of_the_range(drafts, kind):
+    """Weights of one row add up to 1 in the result, whatever they are held as: a value of three quarters of the largest finite one, the
+    same of all tokens, comes out as it is."""
+    p = Drafts([100, 70], drafts, 4, 2, 64, kind=kind, scale=8.0)
+    c = p.cache
+    big = torch.tensor(torch.finfo(DTYPES[kind]).max * 0.75 / (128 if kind == "bf16" else 1)).to(DTYPES[kind])  # (the sum of 100 is held in 32 bits)
+    for r, n in enumerate(c.lens):
+        for t in range(n):
+            c.views[1][c.table[r, t // 16], t % 16] = big
+    c.upload()
+    out, lse, status = p.run()
+    assert status == 0
+    assert bool(((out.double() - big.double()).abs() <= float(big) * (2.0 ** -8 + 2.0 ** -12)).all())
