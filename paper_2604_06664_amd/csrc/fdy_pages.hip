@@ -536,6 +536,8 @@ __global__ void __launch_bounds__(1024) keep_plan_kernel(Keep a) {
 // Where all sources lie behind all places that are written to, every 16-byte word of every token goes by itself, a workgroup
 // kMoved * 256 of a plane's.  Otherwise a lane takes one word of the row's tokens in one plane and moves it for one token after
 // the other, so that a place is read before it is written to: tokens only move to the front.  kSerial of them are under way together.
+// Memory bounds it where many move (1.05 GB read + written 236 us, 4.4 TB/s); few are a chain of the plan, page numbers, words and stores
+// (64 paths of 4 tokens of 2 KiB in 72 planes: 22 us; several planes a workgroup 24, one division of 64 bits less no change).
 constexpr u32 kMoved = 4, kSerial = 16;
 __global__ void __launch_bounds__(256) keep_move_kernel(Keep a) {
   const u32 i = blockIdx.x;

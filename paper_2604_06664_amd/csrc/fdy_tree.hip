@@ -821,7 +821,13 @@ __device__ __forceinline__ void finish_row(const Tree& a, const Seq& q, u32 kv_h
 constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; }  // workgroups of a compute unit
 constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves == 4 ? 3 : 1) : resident(dim, waves); }
 
-// kShared: four waves at least take the same tokens, eight waves a workgroup.
+// kShared: four waves at least take the same tokens, through LDS, four or eight waves a workgroup; otherwise every wave reads for itself.
+// us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 272 (443 TFLOP/s of scores and sums, half as much again
+// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 83 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 185 (4.3 TB/s);
+// one of 517 tokens 21.5, a chain of two launches.  What the first spends: without loads 227, those alone 110, without both 43; without
+// the second part of the weights 42 less, without following the maximum 26 less, without the exponentials 8.  The matrix cores and
+// the vector unit take the sum of their times: products with values beside the next tile's weights in one wave gained nothing
+// (275 for 275), keys a tile ahead in registers neither (283).
 template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves, bool kShared, bool kDirect>
 __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) * kWaves / 4) tree_kernel(Tree a) {
   typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
