@@ -26,7 +26,8 @@ struct TreeArg {
   struct Split* splits;  // [shares]: of the unit that goes on from the share to the next
   float* parts;          // [shares][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
   u32 page_shift, group;
-  u32 beside, fill;  // heads of a token that a workgroup takes at least, if there are so many
+  u32 beside;  // heads of a token that a workgroup takes at least, if there are so many
+  u32 solid, least;  // solid 1: no unit of work is divided; least: places of a share
 };
 typedef Arg<TreeArg> Tree;
 
@@ -41,8 +42,9 @@ struct Seq {
   u32 query, count;  // its first drafted token in q, and how many
   int base;         // tokens ahead of them
   u32 rows, tiles, columns, together, rounds;  // tiles: of a head's rows
+  u32 solid;
   __device__ u32 units() const { return (columns + together - 1) / together; }
-  __device__ u32 unit(u32 each) const { return rounds + each ? rounds + each : 1; }
+  __device__ u32 unit(u32 each) const { return !solid && rounds + each ? rounds + each : 1; }
 };
 __device__ __forceinline__ Seq uniform(const Seq& v) {
   Seq q;
@@ -51,7 +53,7 @@ __device__ __forceinline__ Seq uniform(const Seq& v) {
   q.query = fdy::uniform(v.query), q.count = fdy::uniform(v.count), q.base = (int)fdy::uniform((u32)v.base);
   q.rows = fdy::uniform(v.rows), q.together = fdy::uniform(v.together), q.tiles = fdy::uniform(v.tiles);
   q.columns = fdy::uniform(v.columns);
-  q.rounds = fdy::uniform(v.rounds);
+  q.rounds = fdy::uniform(v.rounds), q.solid = fdy::uniform(v.solid);
   return q;
 }
 
@@ -83,6 +85,7 @@ __device__ __forceinline__ Seq seq_of(const Tree& a, u32 s) {
     while (q.together > 1 && q.together >= 2 * q.columns) q.together /= 2;
   const u32 apart = kWaves / q.together;
   q.rounds = (q.span.tiles() + apart - 1) / apart;
+  q.solid = a.solid;
   return q;
 }
 
@@ -93,7 +96,7 @@ struct TreeShare {
 };
 template <u32 kWaves>
 struct TreeLds {
-  u32 sum[kWaves], seq, start;
+  u32 sum[kWaves], units[kWaves], seq, start;
 };
 
 // All threads of the workgroup.
@@ -102,22 +105,24 @@ __device__ __forceinline__ bool find_tree_share(const Tree& a, TreeShare& out, T
   constexpr u32 kThreads = 64 * kWaves;
   const u32 n = a.d.n_seqs, tid = threadIdx.x, slice = (n + kThreads - 1) / kThreads;
   const u32 s0 = min(tid * slice, n), s1 = min(s0 + slice, n);
-  u32 mine = 0;  // places, without any ahead of rounds
+  u32 mine = 0, units = 0;  // places, without any ahead of rounds
   for (u32 s = s0; s < s1; ++s) {
     const Seq q = seq_of<kRows, kWaves, kLeast>(a, s);
     if (q.span.bad && q.count == 0 && blockIdx.x == 0) raise_status(a.status, FDY_ST_BAD_INDEX);  // no one else looks at it
-    mine += q.units() * q.unit(0);
+    mine += q.units() * q.unit(0), units += q.units();
   }
   const u32 inc = wave_incl_scan(mine);
-  if (lane_id() == 63) lds.sum[tid >> 6] = inc;
+  if (kLeast > 1) units = wave_incl_scan(units);
+  if (lane_id() == 63) lds.sum[tid >> 6] = inc, lds.units[tid >> 6] = units;
   __syncthreads();
   u32 before = inc - mine, total = 0;
+  units = 0;
 #pragma unroll
   for (u32 w = 0; w < kWaves; ++w) {
     if (w < tid >> 6) before += lds.sum[w];
-    total += lds.sum[w];
+    total += lds.sum[w], units += lds.units[w];
   }
-  out.each = fdy::uniform(total <= gridDim.x ? 0 : kEach);
+  out.each = fdy::uniform(total <= gridDim.x || a.solid ? 0 : kEach);
   if (out.each) {
     mine = 0, before = 0, total = 0;
     for (u32 s = s0; s < s1; ++s) {
@@ -142,6 +147,7 @@ __device__ __forceinline__ bool find_tree_share(const Tree& a, TreeShare& out, T
   if (tid == 0) a.splits[out.at].parts = 0;
   if (total == 0) return false;
   out.per = max((total - 1) / g + 1, out.each + 1);
+  if (kLeast > 1 && out.per < a.least) out.per = max(out.per, min(a.least, total / fdy::uniform(units)));  // (no more than units have, on average)
   if ((u64)out.at * out.per >= total) return false;
   out.begin = out.at * out.per;
   out.end = total - out.begin > out.per ? out.begin + out.per : total;
@@ -822,9 +828,9 @@ constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; 
 constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves == 4 ? 3 : 1) : resident(dim, waves); }
 
 // kShared: four waves at least take the same tokens, through LDS, four or eight waves a workgroup; otherwise every wave reads for itself.
-// us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 272 (443 TFLOP/s of scores and sums, half as much again
-// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 83 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 185 (4.3 TB/s);
-// one of 517 tokens 21.5, a chain of two launches.  What the first spends: without loads 227, those alone 110, without both 43; without
+// us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 268 (450 TFLOP/s of scores and sums, half as much again
+// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 82 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 189 (4.2 TB/s);
+// one of 517 tokens 18, a chain.  What the first spends: without loads 227, those alone 110, without both 43; without
 // the second part of the weights 42 less, without following the maximum 26 less, without the exponentials 8.  The matrix cores and
 // the vector unit take the sum of their times: products with values beside the next tile's weights in one wave gained nothing
 // (275 for 275), keys a tile ahead in registers neither (283).
@@ -897,7 +903,8 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
     Sums<T, kDim, kTiles> sums;
     sums.clear();
     const u32 tile0 = q.span.first / kTile, tiles = q.span.tiles();
-    const u32 begin = (lo - start) * apart, end = (hi - start) * apart < tiles ? (hi - start) * apart : tiles;
+    u32 begin = (lo - start) * apart, end = (hi - start) * apart < tiles ? (hi - start) * apart : tiles;
+    if (q.solid) begin = 0, end = tiles;
     if constexpr (kShared) {
       if (q.rounds)
         Way::walk(a, q, head, qs, draft, scale, fdy::uniform(tile0 + begin), fdy::uniform(tile0 + end), apart, turn, works, s_mem, sums, bad);
@@ -1068,17 +1075,30 @@ u64 most_places(const fdy_draft& d, u32 rows) {
 }
 constexpr u32 kMostShares = kCus * 4;
 constexpr size_t kSplitBytes = kMostShares * sizeof(Split);
+constexpr u32 kSolid = 3, kSolidShared = 4;  // tiles of a wave, and of a workgroup that shares them
 
 template <typename T, bool kF8, int kDim>
 int launch_tree(const Tree& a, hipStream_t stream) {
   (void)hipGetLastError();  // drop any stale error left by earlier, unrelated runtime calls
-  auto go = [&](auto kernel, auto join, u32 rows, u32 waves, u32 of_unit) {
+  auto go = [&](auto kernel, auto join, u32 rows, u32 waves, u32 of_unit, u32 solid, bool shared = false) {
     u64 shares = kCus * of_unit;
     const u64 most = most_places(a.d, 16);
     if (shares > most) shares = most;
-    hipLaunchKernelGGL(kernel, dim3((u32)shares), dim3(64 * waves), 0, stream, a);
-    const u32 slices = (rows * waves * (a.d.kv.head_dim / 4) + 255) / 256;  // of 256 items of four elements
-    if (shares > 1) hipLaunchKernelGGL(join, dim3((u32)shares, slices < 16 ? slices : 16), dim3(256), 0, stream, a);
+    // Few units, and none of more rounds than a launch that joins parts is worth: each goes to one workgroup (8 drafted tokens over 517,
+    // three rounds: 18 us, in parts 20; over 1,000, four rounds: 22.8 and 21.3).
+    Tree b = a;
+    const u64 tiles_of = a.d.window && a.d.window < 1u << 30 ? (a.d.window + a.d.max_draft) / kTile + 2 : ~0ull, tiles = row_tiles(a.d);
+    const u64 units = a.d.n_seqs * (u64)a.d.kv.n_heads * ((a.d.max_draft * a.group + rows - 1) / rows);
+    b.solid = units <= shares && (tiles < tiles_of ? tiles : tiles_of) <= solid;
+    if (b.solid) shares = units;
+    // Shares of one or two tiles have more to write and to join than to work on where many rows share a tile: at least four, eight of
+    // long rows (64 drafted tokens over 1,000: one 85 us, four 38, eight 44; over 4,000: four 91, eight 56).
+    b.least = !shared || b.solid ? 1 : tiles > 64 ? 8 : 4;
+    hipLaunchKernelGGL(kernel, dim3((u32)shares), dim3(64 * waves), 0, stream, b);
+    if (b.solid) return;
+    // slices of at least 256 items of four elements (64 drafted tokens over 2,000: 16 of them 52 us, 32 42; 12 such rows 88 and 90)
+    const u32 slices = (rows * waves * (a.d.kv.head_dim / 4) + 255) / 256, most_slices = units <= 256 ? 32 : 16;
+    if (shares > 1) hipLaunchKernelGGL(join, dim3((u32)shares, slices < most_slices ? slices : most_slices), dim3(256), 0, stream, b);
   };
   // 32 rows a wave, 16 where their sums would not fit the registers or where there are no more
   constexpr int kTwo = kDim <= 128 ? 2 : 1, kOnce = kNonTemporal;
@@ -1087,22 +1107,22 @@ int launch_tree(const Tree& a, hipStream_t stream) {
   const bool direct = !kF8 && a.d.kv.head_dim == kDim;
   const bool small = a.d.kv.page_tokens < 16;
   if (small && rows <= 16)
-    go(tree_kernel<T, kF8, kDim, true, 0, 1, 4, false, false>, tree_join_kernel<T, 16, 4, 1>, 16, 4, resident(kDim, 4));
+    go(tree_kernel<T, kF8, kDim, true, 0, 1, 4, false, false>, tree_join_kernel<T, 16, 4, 1>, 16, 4, resident(kDim, 4), kSolid * 4);
   else if (small && rows <= 64 && kDim <= 128)
-    go(tree_kernel<T, kF8, kDim, true, 0, 1, kFew, true, false>, tree_join_kernel<T, 16, kFew, 4>, 16, kFew, resident(kDim, kFew, true));
+    go(tree_kernel<T, kF8, kDim, true, 0, 1, kFew, true, false>, tree_join_kernel<T, 16, kFew, 4>, 16, kFew, resident(kDim, kFew, true), kSolidShared, true);
   else if (small)
-    go(tree_kernel<T, kF8, kDim, true, 0, kTwo, 8, true, false>, tree_join_kernel<T, 16 * kTwo, 8, 4>, 16 * kTwo, 8, resident(kDim, 8, true));
+    go(tree_kernel<T, kF8, kDim, true, 0, kTwo, 8, true, false>, tree_join_kernel<T, 16 * kTwo, 8, 4>, 16 * kTwo, 8, resident(kDim, 8, true), kSolidShared, true);
   else if (rows <= 16)
-    go(tree_kernel<T, kF8, kDim, false, kOnce, 1, kMost, false, false>, tree_join_kernel<T, 16, kMost, 1>, 16, kMost, resident(kDim, kMost));
+    go(tree_kernel<T, kF8, kDim, false, kOnce, 1, kMost, false, false>, tree_join_kernel<T, 16, kMost, 1>, 16, kMost, resident(kDim, kMost), kSolid * kMost);
   else if (rows <= 16 * kTwo)
     go(tree_kernel<T, kF8, kDim, false, kOnce, kTwo, kMost, false, false>, tree_join_kernel<T, 16 * kTwo, kMost, 1>, 16 * kTwo, kMost,
-       resident(kDim, kMost));
+       resident(kDim, kMost), kSolid * kMost);
   else if (rows <= 64 && kDim <= 128)
     go(direct ? tree_kernel<T, kF8, kDim, false, 0, 1, kFew, true, !kF8> : tree_kernel<T, kF8, kDim, false, 0, 1, kFew, true, false>,
-       tree_join_kernel<T, 16, kFew, 4>, 16, kFew, resident(kDim, kFew, true));
+       tree_join_kernel<T, 16, kFew, 4>, 16, kFew, resident(kDim, kFew, true), kSolidShared, true);
   else
     go(direct ? tree_kernel<T, kF8, kDim, false, 0, kTwo, 8, true, !kF8> : tree_kernel<T, kF8, kDim, false, 0, kTwo, 8, true, false>,
-       tree_join_kernel<T, 16 * kTwo, 8, 4>, 16 * kTwo, 8, resident(kDim, 8, true));
+       tree_join_kernel<T, 16 * kTwo, 8, 4>, 16 * kTwo, 8, resident(kDim, 8, true), kSolidShared, true);
   FDY_HIP_TRY(hipGetLastError());
   return FDY_OK;
 }
