@@ -42,9 +42,8 @@ struct Seq {
   u32 query, count;  // its first drafted token in q, and how many
   int base;         // tokens ahead of them
   u32 rows, tiles, columns, together, rounds;  // tiles: of a head's rows
-  u32 solid;
   __device__ u32 units() const { return (columns + together - 1) / together; }
-  __device__ u32 unit(u32 each) const { return !solid && rounds + each ? rounds + each : 1; }
+  __device__ u32 unit(u32 each) const { return rounds + each ? rounds + each : 1; }
 };
 __device__ __forceinline__ Seq uniform(const Seq& v) {
   Seq q;
@@ -53,7 +52,7 @@ __device__ __forceinline__ Seq uniform(const Seq& v) {
   q.query = fdy::uniform(v.query), q.count = fdy::uniform(v.count), q.base = (int)fdy::uniform((u32)v.base);
   q.rows = fdy::uniform(v.rows), q.together = fdy::uniform(v.together), q.tiles = fdy::uniform(v.tiles);
   q.columns = fdy::uniform(v.columns);
-  q.rounds = fdy::uniform(v.rounds), q.solid = fdy::uniform(v.solid);
+  q.rounds = fdy::uniform(v.rounds);
   return q;
 }
 
@@ -85,7 +84,7 @@ __device__ __forceinline__ Seq seq_of(const Tree& a, u32 s) {
     while (q.together > 1 && q.together >= 2 * q.columns) q.together /= 2;
   const u32 apart = kWaves / q.together;
   q.rounds = (q.span.tiles() + apart - 1) / apart;
-  q.solid = a.solid;
+  if (a.solid && q.rounds) q.rounds = 1;  // all of them as one
   return q;
 }
 
@@ -829,7 +828,7 @@ constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves
 
 // kShared: four waves at least take the same tokens, through LDS, four or eight waves a workgroup; otherwise every wave reads for itself.
 // us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 268 (450 TFLOP/s of scores and sums, half as much again
-// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 82 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 189 (4.2 TB/s);
+// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 82 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 185 (4.3 TB/s);
 // one of 517 tokens 18, a chain.  What the first spends: without loads 227, those alone 110, without both 43; without
 // the second part of the weights 42 less, without following the maximum 26 less, without the exponentials 8.  The matrix cores and
 // the vector unit take the sum of their times: products with values beside the next tile's weights in one wave gained nothing
@@ -904,7 +903,7 @@ __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) *
     sums.clear();
     const u32 tile0 = q.span.first / kTile, tiles = q.span.tiles();
     u32 begin = (lo - start) * apart, end = (hi - start) * apart < tiles ? (hi - start) * apart : tiles;
-    if (q.solid) begin = 0, end = tiles;
+    if (a.solid) begin = 0, end = tiles;
     if constexpr (kShared) {
       if (q.rounds)
         Way::walk(a, q, head, qs, draft, scale, fdy::uniform(tile0 + begin), fdy::uniform(tile0 + end), apart, turn, works, s_mem, sums, bad);
