@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -25,11 +27,19 @@ def hipcc():
 
 
 def build_lib(verbose=False):
-    cmd = [hipcc()] + FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    """Each source by itself, as many at once as there are processors (attention's kernels take a minute each), then one link."""
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        def compile_one(s):
+            out = os.path.join(d, s + ".o")
+            cmd = [hipcc()] + [f for f in FLAGS if f != "-shared"] + ["-c", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+            cmd += [os.path.join(CSRC, s), "-o", out]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            subprocess.check_call(cmd)
+            return out
+
+        objects = list(pool.map(compile_one, SOURCES))
+        subprocess.check_call([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", LIB])
     return LIB
 
 
