@@ -827,8 +827,8 @@ constexpr u32 resident(int dim, u32 waves) { return dim <= 128 ? 8 / waves : 1; 
 constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves == 4 ? 3 : 1) : resident(dim, waves); }
 
 // kShared: four waves at least take the same tokens, through LDS, four or eight waves a workgroup; otherwise every wave reads for itself.
-// us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 268 (450 TFLOP/s of scores and sums, half as much again
-// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 82 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 185 (4.3 TB/s);
+// us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 270 (445 TFLOP/s of scores and sums, half as much again
+// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 83 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 185 (4.3 TB/s);
 // one of 517 tokens 18, a chain.  What the first spends: without loads 227, those alone 110, without both 43; without
 // the second part of the weights 42 less, without following the maximum 26 less, without the exponentials 8.  The matrix cores and
 // the vector unit take the sum of their times: products with values beside the next tile's weights in one wave gained nothing
