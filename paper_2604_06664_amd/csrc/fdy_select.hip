@@ -473,7 +473,9 @@ __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
   low = ~wave_incl_most(~low), high = wave_incl_most(high);
   if (l == 63) atomicMin((unsigned long long*)&s_low, low), atomicMax((unsigned long long*)&s_high, high);
   __syncthreads();
-  low = s_low, high = s_high - low;
+  // All of the search is the workgroup's own and stays in scalar registers.  (Not only for speed: with its amounts of shifts in vector
+  // registers the variant that reads keys again had one in the last of 64, and there v_lshlrev_b64 took another register's value.)
+  low = uniform(s_low), high = uniform(s_high) - low;
   // of the keys less `low` those from `bound` + 2^shift on are taken, and of those from `bound` on `left`
   u32 shift = high ? 64 - (u32)__builtin_clzll(high) : 0;
   u64 bound = 0;
@@ -499,13 +501,13 @@ __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
       for (u32 i = tid - 64; i < kBins; i += kThreads - 64) s_bins[turn ^ 1][i] = 0;
     }
     __syncthreads();
-    left -= s_above;
-    bound += (u64)s_bin << below;
+    left -= uniform(s_above);
+    bound += (u64)uniform(s_bin) << below;
     shift = below;
-    if (s_here == left) break;  // all that have these bits are taken
+    if (uniform(s_here) == left) break;  // all that have these bits are taken
   }
   // (what the next turn writes to s_bin it writes behind a barrier that all have come to)
-  const bool some = s_here != left;  // of those equal
+  const bool some = uniform(s_here) != left;  // of those equal
   bound += low;
   const u64 step = shift < 64 ? 1ull << shift : 0, over = bound + step;  // (over 0: behind the last of all keys)
   auto above = [&](u64 key) { return key >= over && over != 0 && shift < 64; };
@@ -560,7 +562,9 @@ __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
       const u64 rank = before + block_excl_scan(x, s_scan, sum);
       before += sum;
       const u32 equals = (u32)(rank >> 32);
-      if (x == 1 || (x && equals < left)) out[sinks + (u32)rank + min(equals, left)] = table[j];
+      const u32 at = (u32)rank + min(equals, left);
+      // (keys are read twice here: whatever became of them meanwhile, nothing is written behind the list)
+      if ((x == 1 || (x && equals < left)) && at < budget - sinks - recent) out[sinks + at] = table[j];
     }
   }
 }

@@ -1,0 +1,49 @@
+"""The library's own kernels as they were compiled: what the sources cannot say and the hardware does not forgive."""
+import os
+import re
+import subprocess
+
+import pytest
+
+import paper_2604_06664_amd as fdy
+
+TOOLS = "/opt/rocm/llvm/bin/"
+MAGIC = b"__CLANG_OFFLOAD_BUNDLE__"
+
+
+def kernels(tmp_path):
+    """(name, disassembly) of every kernel that was built from csrc/."""
+    if not os.path.exists(TOOLS + "llvm-objdump"):
+        pytest.skip("no disassembler")
+    if not os.path.exists(fdy.LIB_PATH):
+        from paper_2604_06664_amd.build import build_lib
+
+        build_lib()
+    fat = str(tmp_path / "fat")
+    subprocess.check_call([TOOLS + "llvm-objcopy", f"--dump-section=.hip_fatbin={fat}", fdy.LIB_PATH, str(tmp_path / "copy")])
+    data = open(fat, "rb").read()
+    at = [m.start() for m in re.finditer(MAGIC, data)]
+    assert at
+    found = []
+    for i, (a, b) in enumerate(zip(at, at[1:] + [len(data)])):
+        bundle, code = str(tmp_path / f"b{i}"), str(tmp_path / f"c{i}")
+        open(bundle, "wb").write(data[a:b])
+        subprocess.check_call([TOOLS + "clang-offload-bundler", "--type=o", "--unbundle", f"--input={bundle}",
+                               "--targets=hipv4-amdgcn-amd-amdhsa--gfx950", f"--output={code}"])
+        text = subprocess.run([TOOLS + "llvm-objdump", "-d", "--no-show-raw-insn", code], check=True, capture_output=True, text=True).stdout
+        found += re.findall(r"^[0-9a-f]+ <(\S+)>:\n(.*?)(?=^[0-9a-f]+ <|\Z)", text, re.S | re.M)
+    return found
+
+
+def test_no_shift_takes_its_amount_from_the_last_register(tmp_path):
+    """A shift of 64 bits by a vector register's amount shifted by another register's where the amount lay in the last one that a wave has
+    (they are given out in eights): of a kernel of 64 registers `v_lshlrev_b64 v[6:7], v63, v[6:7]` shifted by v0 in some of its waves."""
+    found = kernels(tmp_path)
+    assert len(found) > 200
+    wrong = []
+    for name, code in found:
+        used = [int(x) for x in re.findall(r"\bv(\d+)\b", code)] + [int(x) for x in re.findall(r"\bv\[\d+:(\d+)\]", code)]
+        amounts = re.findall(r"v_(?:lshlrev_b64|lshrrev_b64|ashrrev_i64)\S*\s+v\[\d+:\d+\], v(\d+),", code)
+        if used and max(used) % 8 == 7 and str(max(used)) in amounts:
+            wrong.append(name)
+    assert not wrong, wrong
