@@ -509,9 +509,9 @@ __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {
   // (what the next turn writes to s_bin it writes behind a barrier that all have come to)
   const bool some = uniform(s_here) != left;  // of those equal
   bound += low;
-  const u64 step = shift < 64 ? 1ull << shift : 0, over = bound + step;  // (over 0: behind the last of all keys)
-  auto above = [&](u64 key) { return key >= over && over != 0 && shift < 64; };
-  auto equal = [&](u64 key) { return key >= bound && !above(key); };
+  // (a difference, for bound + 2^shift may lie behind the last of all keys)
+  auto above = [&](u64 key) { return key >= bound && (key - bound) >> shift; };
+  auto equal = [&](u64 key) { return key >= bound && !((key - bound) >> shift); };
   if constexpr (kMine > 0) {
     // a bit for each page that is taken, with the sums ahead of each word; then every place of the list looks for its page
     u32 rank = 0;

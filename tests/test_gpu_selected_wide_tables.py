@@ -1,5 +1,7 @@
 """fdy_page_select over wide tables: choices equal to the oracle's, whatever the table's width has each thread hold of a row's keys, and
 nothing written outside the lists."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -77,3 +79,16 @@ def test_long_and_short_rows(width, kind):
 @pytest.mark.parametrize("sinks,recent,budget", [(0, 1, 1), (0, 1, 2), (5, 7, 12), (5, 7, 13), (0, 600, 1200), (700, 1, 1300), (0, 1, 1999)])
 def test_shares_of_the_list(sinks, recent, budget, width):
     choose([scores_of(MIXED, 2000), scores_of(KINDS, 1500)], width, budget, sinks, recent, pt=4)
+
+
+@pytest.mark.parametrize("odd", [1, 12, 13, 14, 40])
+@pytest.mark.parametrize("special", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("kind", [POSITIVE, NEGATIVE])
+@pytest.mark.parametrize("width", [2049, 8193, 16385])
+def test_pages_of_the_largest_and_smallest_keys(width, kind, special, odd):
+    """13 places beside the last page's, and fewer, as many and more pages whose score is no number or infinite: the key of a score that
+    is no number is the last of all 64-bit integers."""
+    x = scores_of(kind, 900, odd)
+    x[np.random.default_rng(odd).permutation(899)[:odd]] = special
+    choose([x, x[:100].copy()], width, 14)
+    choose([x, x[:100].copy()], width, odd + 1 + (special == -math.inf), 1, 1)
