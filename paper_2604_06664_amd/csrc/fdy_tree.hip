@@ -389,7 +389,7 @@ struct Alone {
       x.load_k(a, z, q.span, ids_next, t_next, bad);
       bool odd = false;
       u32 there = 0;
-      if (!(Tl::whole(ids) && (int)(t + kTile) <= past && (int)t >= opens)) {
+      if (!(Tl::whole(ids) && (int)(t + kTile - 1) < past && (int)t >= opens)) {  // (t + kTile may be 2^31)
         u32 any = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) there |= x.seen(a, z, q.span, ids, t, j / 4, j % 4) ? 1u << j : 0;
@@ -792,7 +792,7 @@ struct Together {
         const uint8_t* k = lds + slot * kSlot + mine * kTileBytes;
         f32x4 s[kTiles][2];
         const u32 first = tile * kTile;
-        if (all_there(pages, n) && (int)(first + n * kTile) <= q.base && (int)first >= opens) {
+        if (all_there(pages, n) && (int)(first + n * kTile - 1) < q.base && (int)first >= opens) {  // (the sum may be 2^31)
           score(k, qs, s);
           u32 i = mine;
           for (; i + apart < n; i += apart, k += apart * kTileBytes)
