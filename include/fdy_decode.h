@@ -221,7 +221,8 @@ int fdy_tree_attention(const fdy_draft* h_desc, void* d_workspace, size_t worksp
  * different lengths share get the bounds of either.  fresh[s] < 0 or > max_fresh: held within, FDY_ST_BAD_INDEX; rows, lens,
  * page numbers out of range: as fdy_paged_attention.  kv.v is not read.
  *   bounds and kv.k 16-byte aligned, kv's strides multiples of 16 bytes, head_dim of 16 bytes' elements; n_seqs <= 65,536,
- *   row_pages * page_tokens < 2^31. */
+ *   row_pages * page_tokens < 2^31, the pages of a sequence that may have new tokens (min(row_pages, (max_fresh - 1) / page_tokens
+ *   + 2), max_fresh 1 with fresh NULL) times kv.n_heads < 2^31. */
 typedef struct {
   void* bounds;         /* [kv.n_pages][kv.n_heads][2][head_dim], of kv.type */
   const int32_t* table; /* [n_rows][row_pages] */

@@ -577,8 +577,15 @@ int go(F kernel, dim3 grid, u32 threads, void* stream, const A& a) {
   return FDY_OK;
 }
 
+// Pages of a sequence that have new tokens, at most.
+u32 slots_of(const fdy_bounds& d) {
+  const u32 fresh = d.fresh && d.max_fresh ? d.max_fresh : 1, slots = (fresh - 1) / d.kv.page_tokens + 2;
+  return slots < d.row_pages ? slots : d.row_pages ? d.row_pages : 1;
+}
+
 bool bounds_valid(const fdy_bounds& d) {
   if (!kv_valid(d.kv) || d.n_seqs > 65536u || (u64)d.row_pages * d.kv.page_tokens >> 31) return false;
+  if ((u64)slots_of(d) * d.kv.n_heads >> 31) return false;
   const u32 per = d.kv.type == FDY_F8 ? 16 : 8;
   return d.kv.head_dim % per == 0 && (d.kv.page_stride | d.kv.token_stride | d.kv.head_stride) % per == 0;
 }
@@ -608,9 +615,7 @@ extern "C" int fdy_page_bounds(const fdy_bounds* h, uint32_t* d_status, void* st
   a.status = d_status;
   a.shift = log2_of(d.kv.page_tokens);
   a.lanes = up_to_power(d.kv.head_dim / (d.kv.type == FDY_F8 ? 16 : 8));
-  const u32 fresh = d.max_fresh ? d.max_fresh : 1;
-  a.slots = (fresh - 1) / d.kv.page_tokens + 2;
-  if (a.slots > d.row_pages) a.slots = d.row_pages ? d.row_pages : 1;
+  a.slots = slots_of(d);
   const u64 blocks = ((u64)a.slots * d.kv.n_heads + 3) / 4;
   const dim3 grid(d.n_seqs, (u32)(blocks < 32768 ? blocks : 32768));
   if (d.kv.type == FDY_BF16) return go(bounds_kernel<FDY_BF16>, grid, 256, stream, a);
