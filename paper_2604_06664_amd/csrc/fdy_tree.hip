@@ -571,7 +571,8 @@ struct Together {
       }
   }
   // The same to LDS, 1 KiB of it from `slot` on for each piece.  (Written as it stands since the compiler has every later read of LDS wait
-  // for such loads, whichever slot it is of; the workgroup's barrier behind arrived() is what orders them.)
+  // for such loads, whichever slot it is of; the workgroup's barrier behind arrived() is what orders them.  m0 is the compiler's own and
+  // is not taken as one of a statement's clobbers: no other instruction of these kernels may use it, which a test of the compiled code holds.)
   __device__ __forceinline__ void bring(const Tree& a, u32 of_head, u32 wave, u32 tile, u32 n, const Ids& ids, u32 slot) const {
     const u64 page_bytes = a.d.kv.page_stride * kEs;
     const u32 token_bytes = (u32)a.d.kv.token_stride * kEs;
