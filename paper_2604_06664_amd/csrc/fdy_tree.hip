@@ -26,16 +26,15 @@ struct TreeArg {
   struct Split* splits;  // [shares]: of the unit that goes on from the share to the next
   float* parts;          // [shares][2] of: [rows][head_dim] sums, [rows] pairs of a maximum and a sum of e; 16-byte aligned
   u32 page_shift, group;
-  u32 beside;  // heads of a token that a workgroup takes at least, if there are so many
   u32 solid, least;  // solid 1: no unit of work is divided; least: places of a share
 };
 typedef Arg<TreeArg> Tree;
 
 // ---- which work a workgroup takes -------------------------------------------------------------------
 // The query rows of a cache head (drafted tokens x query heads) are tiles of kRows; all heads' tiles one after the other are the
-// columns of a sequence.  `together` waves take as many columns side by side: all of a head, which read the same, and of neighbouring
-// heads where these lie beside each other in a token; the waves that are left over take other tokens: `apart` tiles of 32 a round.
-// A unit is one such group of columns of one sequence; units lie one after the other on a line, kEach places and then a place for
+// columns of a sequence.  `together` waves take as many columns of a head side by side, which read the same (kLeast of them at least; with
+// kLeast 1, where every wave reads for itself, a head has one column), and the workgroup's other waves other tokens: `apart` tiles of 32 a
+// round.  A unit is one such group of columns of one sequence; units lie one after the other on a line, kEach places and then a place for
 // every round, and equal shares of the line go to the workgroups.  Where there is a workgroup for every round, each takes one.
 struct Seq {
   Span span;        // tokens that any of its queries sees
@@ -76,12 +75,11 @@ __device__ __forceinline__ Seq seq_of(const Tree& a, u32 s) {
   q.rows = q.count * a.group;
   q.tiles = (q.rows + kRows - 1) / kRows;
   q.together = kLeast;
-  const u32 most = kLeast == 1 && a.beside > q.tiles ? a.beside : q.tiles;
-  while (q.together < kWaves && q.together < most) q.together *= 2;
-  if (kLeast > 1) q.tiles = (q.tiles + q.together - 1) / q.together * q.together;  // a group's are of one head
+  if (kLeast > 1) {
+    while (q.together < kWaves && q.together < q.tiles) q.together *= 2;
+    q.tiles = (q.tiles + q.together - 1) / q.together * q.together;  // a group's are of one head
+  }
   q.columns = q.tiles * a.d.kv.n_heads;
-  if (kLeast == 1)
-    while (q.together > 1 && q.together >= 2 * q.columns) q.together /= 2;
   const u32 apart = kWaves / q.together;
   q.rounds = (q.span.tiles() + apart - 1) / apart;
   if (a.solid && q.rounds) q.rounds = 1;  // all of them as one
@@ -1174,7 +1172,6 @@ extern "C" int fdy_tree_attention(const fdy_draft* h, void* d_workspace, size_t 
   a.parts = (float*)((uint8_t*)d_workspace + kSplitBytes);
   a.page_shift = log2_of(d.kv.page_tokens);
   a.group = d.n_q_heads / d.kv.n_heads;
-  a.beside = 1;
   const bool f8 = d.kv.type == FDY_F8;
   if (d.type == FDY_BF16)
     return f8 ? launch_tree<Bf16, true>(a, (hipStream_t)stream) : launch_tree<Bf16, false>(a, (hipStream_t)stream);
