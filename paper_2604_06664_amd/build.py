@@ -45,7 +45,7 @@ def build_lib(verbose=False):
 
 TOY_SRC = [os.path.join(ROOT, "tests", "toy_graph", f) for f in ("toy_graph.hip", "install_scale.hip",
                                                                 "arena_graph.hip", "hold_units.hip",
-                                                                "decode_graph.hip")]
+                                                                "decode_graph.hip", "draft_graph.hip")]
 TOY_LIB = os.path.join(ROOT, "tests", "toy_graph", "libtoy_graph.so")
 
 
