@@ -221,6 +221,8 @@ int fdy_tree_attention(const fdy_draft* h_desc, void* d_workspace, size_t worksp
  * min(fresh[s], lens[r]) tokens of row r = rows[s] lies (fresh NULL: 1 each); other pages' bounds stay.  Pages that rows of
  * different lengths share get the bounds of either.  fresh[s] < 0 or > max_fresh: held within, FDY_ST_BAD_INDEX; rows, lens,
  * page numbers out of range: as fdy_paged_attention.  kv.v is not read.
+ * Bounds belong to page numbers.  A page that fdy_pages_extend copies holds a new token; after fdy_pages_keep the last kept + 1
+ * tokens of a row lie in all pages that it changed; where fdy_pages_compact moved pages bounds follow by its d_map.
  *   bounds and kv.k 16-byte aligned, kv's strides multiples of 16 bytes, head_dim of 16 bytes' elements; n_seqs <= 65,536,
  *   row_pages * page_tokens < 2^31, the pages of a sequence that may have new tokens (min(row_pages, (max_fresh - 1) / page_tokens
  *   + 2), max_fresh 1 with fresh NULL) times kv.n_heads < 2^31. */
