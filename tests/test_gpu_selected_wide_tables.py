@@ -92,3 +92,8 @@ def test_pages_of_the_largest_and_smallest_keys(width, kind, special, odd):
     x[np.random.default_rng(odd).permutation(899)[:odd]] = special
     choose([x, x[:100].copy()], width, 14)
     choose([x, x[:100].copy()], width, odd + 1 + (special == -math.inf), 1, 1)
+
+
+@pytest.mark.parametrize("width,budget", [(40, 40), (40, 41), (40, 500), (41, 40), (2049, 2048), (2049, 2049), (16385, 16384), (16385, 16400)])
+def test_lists_as_long_as_tables(width, budget):
+    choose([scores_of(MIXED, width), scores_of(MIXED, 40, 2), scores_of(MIXED, 0), scores_of(EQUAL, width - 1)], width, budget)
