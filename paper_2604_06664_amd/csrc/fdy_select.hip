@@ -89,7 +89,8 @@ typedef Arg<BoundsArg> Bounds;
 
 // A wave takes one head of one page: 64 / lanes tokens at a time, kAhead loads of a lane under way, then the lanes that hold the same
 // elements of different tokens are joined.  Tokens behind the last are the last once more.  Memory bounds it: prompts of 131,000 tokens, 8
-// heads of 128, 43 us, 6.2 TB/s; a step of 256 rows 4.5, a launch and two dependent loads.
+// heads of 128, 53 us, 5.0 TB/s (again over the same 267 MB, part of which the card's cache then holds, 43); a step of 256 rows 4.4, a
+// launch and two dependent loads.
 template <int kType>
 __global__ void __launch_bounds__(256) bounds_kernel(Bounds a) {
   constexpr int kE = kElems<kType>, kAhead = 4;
@@ -403,8 +404,9 @@ __global__ void __launch_bounds__(256, kResident<kType>) scores_kernel(Select a)
 // ---- choice -----------------------------------------------------------------------------------------
 // One workgroup for a cache head of a sequence: the key that the last one taken has, ten bits at a time from the highest in which
 // the keys differ, then those above it and as many of those equal to it as there is room for, in the order of the row.
-// kMine: keys that a thread holds in registers, every kThreads-th of the row; 0: keys are read again from the workspace, for rows of
-// more pages.  8,192 pages of 8 heads 13 us: a chain of two or three turns, three barriers each; 768 lists of 4,096 pages 13.
+// kMine: keys that a thread holds in registers, every kThreads-th of the row; 0: keys are read again from the workspace, for tables
+// of more pages (rows' lengths are not known at the launch).  8,192 pages of 8 heads 13 us: a chain of two or three turns, three barriers each;
+// 768 lists of 4,096 pages 13.  Scores and choice of 8,192 pages under a table of 16,384 23 us, of 16,385 39.
 constexpr u32 kThreads = 512, kWaves = kThreads / 64, kBits = 10, kBins = 1u << kBits;
 template <u32 kMine>
 __global__ void __launch_bounds__(kThreads) choice_kernel(Select a) {

@@ -469,7 +469,7 @@ struct Alone {
 //
 // kDirect: straight from the pages to LDS, which 16-bit elements and heads of exactly kDim allow.  kSmall: pages of less than 16 tokens;
 // a wave looks up the page of every token of a stage, a lane each, and hands them to the lanes that read (248 rows a head over pages of 8
-// tokens, 16 rows of 5,319: 433 us where every 16 rows read for themselves, 147 so).
+// tokens, 16 rows of 5,319: 433 us where every 16 rows read for themselves, 144 so).
 template <typename T, bool kF8, int kDim, int kTiles, bool kDirect, u32 kWaves, bool kSmall>
 struct Together {
   typedef typename T::x8 x8;
@@ -827,11 +827,12 @@ constexpr u32 resident(int dim, u32 waves, bool shared) { return shared ? (waves
 
 // kShared: four waves at least take the same tokens, through LDS, four or eight waves a workgroup; otherwise every wave reads for itself.
 // us with both launches: 8 rows of 6,000 to 8,192 tokens, 512 query rows a head 270 (445 TFLOP/s of scores and sums, half as much again
-// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 83 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 185 (4.3 TB/s);
-// one of 517 tokens 18, a chain.  What the first spends: without loads 227, those alone 110, without both 43; without
-// the second part of the weights 42 less, without following the maximum 26 less, without the exponentials 8.  The matrix cores and
-// the vector unit take the sum of their times: products with values beside the next tile's weights in one wave gained nothing
-// (275 for 275), keys a tile ahead in registers neither (283).
+// done, for weights go in two parts); 33 of up to 8,192, 64 query rows 83 (3.1 TB/s); 64 windows of 2,048 in 8 bits, 5 rows 180 (4.4 TB/s);
+// one of 517 tokens 16.5, a chain.  What the first spends: without loads 227, those alone 110, without both 43; without
+// the second part of the weights 42 less, without following the maximum 26 less, without the exponentials 8; products with values beside
+// the next tile's weights in one wave gained nothing (275 for 275), keys a tile ahead in registers neither (283).
+// Its loads are not hidden: variants of 32 rows a wave keep 8 registers in scratch memory (20 to 38 with 8-bit caches, small pages or heads
+// that are not exactly kDim; heads of more than 128 8 to 25), and a wait for one of them back is a wait for all loads, the next stage's too.
 template <typename T, bool kF8, int kDim, bool kSmall, int kPolicy, int kTiles, u32 kWaves, bool kShared, bool kDirect>
 __global__ void __launch_bounds__(64 * kWaves, resident(kDim, kWaves, kShared) * kWaves / 4) tree_kernel(Tree a) {
   typedef Tile<T, kF8, kDim, kSmall, kPolicy> Tl;
@@ -1083,7 +1084,7 @@ int launch_tree(const Tree& a, hipStream_t stream) {
     const u64 most = most_places(a.d, 16);
     if (shares > most) shares = most;
     // Few units, and none of more rounds than a launch that joins parts is worth: each goes to one workgroup (8 drafted tokens over 517,
-    // three rounds: 18 us, in parts 20; over 1,000, four rounds: 22.8 and 21.3).
+    // three rounds: 16.4 us, in parts 18.4; over 1,000, four rounds: 21.4 and 20.0).
     Tree b = a;
     const u64 tiles_of = a.d.window && a.d.window < 1u << 30 ? (a.d.window + a.d.max_draft) / kTile + 2 : ~0ull, tiles = row_tiles(a.d);
     const u64 units = a.d.n_seqs * (u64)a.d.kv.n_heads * ((a.d.max_draft * a.group + rows - 1) / rows);
